@@ -16,3 +16,18 @@ def Translator(*args, **kwargs):
 def make_config(*args, **kwargs):
     from .translator import make_config as _m
     return _m(*args, **kwargs)
+
+
+def F8Weights(*args, **kwargs):
+    from .ops import F8Weights as _w
+    return _w(*args, **kwargs)
+
+
+def LogitRules(*args, **kwargs):
+    from .ops import LogitRules as _r
+    return _r(*args, **kwargs)
+
+
+def constrain(*args, **kwargs):
+    from .ops import constrain as _c
+    return _c(*args, **kwargs)

@@ -15,6 +15,7 @@ ONMT_VALIDATE_HOST, ONMT_VALIDATE_DEVICE = 0, 1
 KERNEL_KINDS = {"generator": 0, "lstm": 1, "attention": 2, "output": 3, "beam_step": 4}
 KERNEL_ALL = (1 << len(KERNEL_KINDS)) - 1
 NOALLOC_SCRATCH_BYTES = 16 << 20
+ONMT_F32, ONMT_BF16, ONMT_F16 = 0, 1, 2
 ERROR_NAMES = {ONMT_EINVAL: "EINVAL", ONMT_ESIZE: "ESIZE", ONMT_EDEVICE: "EDEVICE", ONMT_EUNSUPPORTED: "EUNSUPPORTED"}
 
 
@@ -31,6 +32,13 @@ class OnmtSearchParams(ctypes.Structure):
 
 class OnmtTrace(ctypes.Structure):
     _fields_ = [("slot", c_void_p), ("tok", c_void_p), ("cand", c_void_p), ("steps", c_void_p)]
+
+
+class OnmtLogitRules(ctypes.Structure):
+    _fields_ = [("history", c_void_p), ("history_len", c_void_p), ("history_stride", c_int64), ("max_history", c_int),
+                ("no_repeat_ngram", c_int), ("repetition", c_void_p), ("presence", c_void_p), ("frequency", c_void_p),
+                ("bias_ids", c_void_p), ("bias", c_void_p), ("bias_stride", c_int64), ("n_bias", c_int),
+                ("n_masks", c_int), ("mask", c_void_p), ("mask_stride", c_int64), ("mask_row", c_void_p)]
 
 
 # name -> (restype, argtypes), the full exported surface of include/onmt.h
@@ -62,6 +70,15 @@ SIGNATURES = {
     "onmt_device_status": (c_int, [c_void_p, POINTER(c_int)]),
     "onmt_decode_step_noalloc": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
                                          c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "onmt_f8_bytes": (c_size_t, [c_int, c_int]),
+    "onmt_f8_pack": (c_int, [c_void_p, c_int, c_int64, c_int, c_int, c_void_p, c_size_t, c_void_p]),
+    "onmt_f8_unpack": (c_int, [c_void_p, c_size_t, c_int, c_int, c_void_p, c_int64, c_void_p]),
+    "onmt_f8_linear_ws_bytes": (c_size_t, [c_int, c_int]),
+    "onmt_f8_linear": (c_int, [c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_int, c_int, c_void_p, c_void_p,
+                               c_int, c_int64, c_void_p, c_size_t, c_void_p]),
+    "onmt_constrain_ws_bytes": (c_size_t, [c_int, c_int, c_int, c_int]),
+    "onmt_constrain": (c_int, [POINTER(OnmtLogitRules), c_void_p, c_int, c_int64, c_int, c_int, c_int, c_int, c_void_p,
+                               c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "onmt_profile_enable": (c_int, [c_void_p, c_int, c_uint]),
     "onmt_profile_read": (c_int, [c_void_p, POINTER(c_int), POINTER(c_double), c_int]),
     "onmt_profile_read_kernel": (c_int, [c_void_p, c_int, POINTER(c_int), POINTER(c_double), c_int]),

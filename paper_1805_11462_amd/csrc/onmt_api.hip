@@ -1108,7 +1108,7 @@ GenPartials gen_partials(const GenParams& gp) {
 // mode 0: logp [N, V] full log-softmax; mode 1: top-K (logp [N, K], ids [N, K]); mode 2 (beam search):
 // stop after the generator, leaving its per-tile partials in the step workspace for the beam step;
 // mode 3 (teacher forcing): stop after the attentional vector (out.feed), the generator runs later over
-// all steps at once.
+// all steps at once; mode 4: logp [N, V] = the logits.
 // Optional work of a decoder step beyond the log-distribution.
 struct StepExtras {
   const int32_t* want = nullptr;        // the logit of column want[r] of every row goes to want_logit[r]
@@ -1214,9 +1214,10 @@ int decode_compute(onmt_model* m, const EncWs& w, int B, int S, int K, const Sta
     gp.ntiles = sw.ntiles;
     gp.pmax = sw.pmax;
     gp.psum = sw.psum;
-    gp.logits = mode == 0 ? logp : sw.logits;
-    gp.ld_logits = mode == 0 ? d.Vt : sw.ld_logits;
-    gp.pval = mode == 0 ? nullptr : sw.pval;
+    const bool whole = mode == 0 || mode == 4;
+    gp.logits = whole ? logp : sw.logits;
+    gp.ld_logits = whole ? d.Vt : sw.ld_logits;
+    gp.pval = whole ? nullptr : sw.pval;
     gp.pid = sw.pid;
     gp.want = ex.want;
     gp.want_logit = ex.want_logit;
@@ -1230,7 +1231,7 @@ int decode_compute(onmt_model* m, const EncWs& w, int B, int S, int K, const Sta
     HIP_TRY(gemm_gen(Split16{out.feed16, N, d.kb(d.H)}, m->W_s, d.wterms, gp, st));
     if (timing) time_end(m, st);
   }
-  if (mode == 2) return ONMT_OK;
+  if (mode == 2 || mode == 4) return ONMT_OK;
   float* lse_out = lse ? lse : sw.lse;
   if (mode == 0) {
     HIP_TRY(log_probs(logp, d.Vt, part, N, lse_out, st));
@@ -1247,6 +1248,80 @@ int check_beam(const onmt_model* m, int S, int K) {
   if (attention_lds_bytes(S, m->d.H, K) > 64 * 1024)
     return fail(ONMT_EUNSUPPORTED, "beam * max(hidden, S_max) too large for the attention workgroups");
   return ONMT_OK;
+}
+
+// ------------------------------------------------------------------ matrices of a caller's type, rules on logits
+constexpr int64_t kF8MaxBlocks = 1 << 24;
+constexpr int kMaxRuleVocab = 1 << 20;
+
+int64_t f8_blocks(int64_t rows, int64_t cols) { return ((rows + 15) / 16) * ((cols + kF8Block - 1) / kF8Block); }
+size_t elem_bytes(int dtype) { return dtype == ONMT_F32 ? 4 : 2; }
+
+// Device bytes [lo, hi).
+struct Span {
+  uintptr_t lo, hi;
+  bool meets(const Span& o) const { return lo < o.hi && o.lo < hi; }
+};
+Span span(const void* p, int dtype, int64_t ld, int rows, int cols) {
+  return Span{(uintptr_t)p, (uintptr_t)p + ((uint64_t)(rows - 1) * ld + cols) * elem_bytes(dtype)};
+}
+
+int check_matrix(const char* name, const void* p, int dtype, int64_t ld, int rows, int cols) {
+  if (!p) return fail(ONMT_EINVAL, "%s is NULL", name);
+  if (dtype < ONMT_F32 || dtype > ONMT_F16) return fail(ONMT_EINVAL, "%s has an unknown type %d", name, dtype);
+  if (rows < 1 || cols < 1) return fail(ONMT_EINVAL, "%s needs at least one row and column", name);
+  if (ld < cols) return fail(ONMT_EINVAL, "%s has row stride %lld for %d columns", name, (long long)ld, cols);
+  if (ld > ((int64_t)1 << 44) / rows) return fail(ONMT_EINVAL, "%s spans more than 2^44 elements", name);
+  if ((uintptr_t)p % elem_bytes(dtype)) return fail(ONMT_EINVAL, "%s is not aligned to its elements", name);
+  return ONMT_OK;
+}
+
+int check_packed(const void* packed, size_t bytes, int rows, int cols) {
+  if (!packed || (uintptr_t)packed % 16) return fail(ONMT_EINVAL, "packed must be a 16-byte aligned device buffer");
+  if (rows < 1 || cols < 1) return fail(ONMT_EINVAL, "a packed matrix needs at least one row and column");
+  if (f8_blocks(rows, cols) > kF8MaxBlocks) return fail(ONMT_EUNSUPPORTED, "a matrix of %d x %d is too large", rows, cols);
+  const size_t need = f8_data_bytes(rows, cols) + f8_exp_bytes(rows, cols);
+  if (bytes < need) return fail(ONMT_ESIZE, "packed holds %zu bytes, %zu are needed", bytes, need);
+  return ONMT_OK;
+}
+
+int check_rules(const onmt_logit_rules& q, int N, int V, LogitRules* r) {
+  if (q.history) {
+    if (!q.history_len) return fail(ONMT_EINVAL, "history_len is NULL");
+    if (q.max_history < 1 || q.history_stride < q.max_history) return fail(ONMT_EINVAL, "history needs 1 <= max_history <= history_stride");
+  }
+  if (q.no_repeat_ngram < 0) return fail(ONMT_EINVAL, "no_repeat_ngram must be >= 0");
+  if (q.n_bias < 0) return fail(ONMT_EINVAL, "n_bias must be >= 0");
+  if (q.n_bias > 0 && (!q.bias_ids || !q.bias || q.bias_stride < q.n_bias))
+    return fail(ONMT_EINVAL, "a bias list needs bias_ids, bias and bias_stride >= n_bias");
+  if (q.mask && (q.n_masks < 1 || q.mask_stride < (V + 31) / 32 || (!q.mask_row && q.n_masks < N)))
+    return fail(ONMT_EINVAL, "masks need mask_stride >= ceil(V / 32) and n_masks >= 1 (>= N without mask_row)");
+  const void* words[] = {q.history, q.history_len, q.repetition, q.presence, q.frequency, q.bias_ids, q.bias, q.mask, q.mask_row};
+  for (const void* p : words)
+    if ((uintptr_t)p % 4) return fail(ONMT_EINVAL, "an array of the rules is not aligned to its elements");
+  *r = LogitRules{q.history, q.history_len, q.history_stride, q.max_history, q.repetition, q.presence, q.frequency, q.no_repeat_ngram,
+                  q.bias_ids, q.bias, q.bias_stride, q.n_bias, q.mask, q.mask_stride, q.n_masks, q.mask_row};
+  return ONMT_OK;
+}
+
+size_t constrain_layout(int N, int V, int K, char* base, GenPartials* p) {
+  Carver c;
+  c.base = base;
+  const int nt = (V + kRuleTile - 1) / kRuleTile;
+  const size_t n = (size_t)N * nt;
+  float* pmax = c.take<float>(n);
+  float* psum = c.take<float>(n);
+  float* pval = K > 0 ? c.take<float>(n * K) : nullptr;
+  int32_t* pid = K > 0 ? c.take<int32_t>(n * K) : nullptr;
+  if (p) {
+    p->pmax = pmax;
+    p->psum = psum;
+    p->pval = pval;
+    p->pid = pid;
+    p->ntiles = nt;
+    p->V = V;
+  }
+  return c.off;
 }
 
 }  // namespace
@@ -1306,7 +1381,8 @@ int onmt_decode_step(onmt_model* m, const void* enc_ws, int B, int S, int K, con
   int rc = check_beam(m, S, K);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, K, 0))) return rc;
-  if (mode != 0 && mode != 1) return fail(ONMT_EINVAL, "mode must be 0 (full) or 1 (top-K)");
+  if (mode < 0 || mode > 2) return fail(ONMT_EINVAL, "mode must be 0 (full), 1 (top-K) or 2 (logits)");
+  if (mode == 2 && lse) return fail(ONMT_EINVAL, "lse must be NULL in mode 2");
   if (mode == 1 && !ids) return fail(ONMT_EINVAL, "ids is NULL in top-K mode");
   if (step_ws_bytes < step_layout(m->d, B, S, K, nullptr, nullptr)) return fail(ONMT_ESIZE, "step workspace too small");
   hipStream_t st = (hipStream_t)stream;
@@ -1340,7 +1416,7 @@ int onmt_decode_step(onmt_model* m, const void* enc_ws, int B, int S, int K, con
   parent = parent ? sw.par_s : nullptr;
   EncWs w;
   enc_layout(m->d, B, S, (char*)enc_ws, &w);
-  rc = decode_compute(m, w, B, S, K, si, so, prev_tok, parent, mode, logp, ids, lse, attn, sw, st);
+  rc = decode_compute(m, w, B, S, K, si, so, prev_tok, parent, mode == 2 ? 4 : mode, logp, ids, lse, attn, sw, st);
   if (m->prof) {
     HIP_TRY(hipStreamSynchronize(st));
     time_collect(m);
@@ -1365,7 +1441,8 @@ int onmt_decode_step_noalloc(onmt_model* m, const void* enc_ws, int B, int S, in
   int rc = check_beam(m, S, K);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, K, 0))) return rc;
-  if (mode != 0 && mode != 1) return fail(ONMT_EINVAL, "mode must be 0 (full) or 1 (top-K)");
+  if (mode < 0 || mode > 2) return fail(ONMT_EINVAL, "mode must be 0 (full), 1 (top-K) or 2 (logits)");
+  if (mode == 2 && lse) return fail(ONMT_EINVAL, "lse must be NULL in mode 2");
   if (mode == 1 && !ids) return fail(ONMT_EINVAL, "ids is NULL in top-K mode");
   const size_t bytes = step_layout(m->d, B, S, K, nullptr, nullptr, true), rows = (size_t)B * K;
   const size_t need = bytes - align_up(split16_bytes(rows, m->d.kb(m->d.Hm), 2)) +
@@ -1387,8 +1464,8 @@ int onmt_decode_step_noalloc(onmt_model* m, const void* enc_ws, int B, int S, in
   si = step_input(m->d, si, so);
   HIP_TRY(prepare_step(decode_state(m->d, si, N), split_state(m->d), prev_tok, parent, m->cfg.tgt_vocab, sw.tok_s,
                        sw.par_s, m->err_host, st));
-  return decode_compute(m, w, B, S, K, si, so, sw.tok_s, parent ? sw.par_s : nullptr, mode, logp, ids, lse, attn, sw,
-                        st, StepExtras{}, false);
+  return decode_compute(m, w, B, S, K, si, so, sw.tok_s, parent ? sw.par_s : nullptr, mode == 2 ? 4 : mode, logp, ids,
+                        lse, attn, sw, st, StepExtras{}, false);
 }
 
 int onmt_device_status(onmt_model* m, int* code) {
@@ -1625,6 +1702,96 @@ int onmt_score(onmt_model* m, const int32_t* src, const int32_t* len, int B, int
   HIP_TRY(hipMemcpyAsync(out_nll, w.nll, sizeof(double) * B, hipMemcpyDeviceToDevice, st));
   HIP_TRY(hipStreamSynchronize(st));
   if (m->prof) time_collect(m);
+  return ONMT_OK;
+}
+
+size_t onmt_f8_bytes(int rows, int cols) {
+  if (f8_blocks(rows, cols) > kF8MaxBlocks || rows < 1 || cols < 1) return 0;
+  return f8_data_bytes(rows, cols) + f8_exp_bytes(rows, cols);
+}
+
+int onmt_f8_pack(const void* w, int dtype, int64_t ld, int rows, int cols, void* packed, size_t packed_bytes, void* stream) {
+  int rc = check_matrix("w", w, dtype, ld, rows, cols);
+  if (rc || (rc = check_packed(packed, packed_bytes, rows, cols))) return rc;
+  HIP_TRY(f8_pack(w, dtype, ld, rows, cols, f8_mat(packed, rows, cols), (hipStream_t)stream));
+  return ONMT_OK;
+}
+
+int onmt_f8_unpack(const void* packed, size_t packed_bytes, int rows, int cols, float* out, int64_t ld_out, void* stream) {
+  int rc = check_matrix("out", out, ONMT_F32, ld_out, rows, cols);
+  if (rc || (rc = check_packed(packed, packed_bytes, rows, cols))) return rc;
+  HIP_TRY(f8_unpack(f8_mat((void*)packed, rows, cols), rows, cols, out, ld_out, (hipStream_t)stream));
+  return ONMT_OK;
+}
+
+size_t onmt_f8_linear_ws_bytes(int M, int cols) {
+  if (f8_blocks(M, cols) > kF8MaxBlocks || M < 1 || cols < 1) return 0;
+  return f8_linear_ws(M, cols);
+}
+
+int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* packed, size_t packed_bytes, int rows, int cols,
+                   const float* bias, void* out, int out_dtype, int64_t ld_out, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_matrix("x", x, dtype, ldx, M, cols);
+  if (rc || (rc = check_matrix("out", out, out_dtype, ld_out, M, rows)) || (rc = check_packed(packed, packed_bytes, rows, cols)))
+    return rc;
+  if ((uintptr_t)bias % sizeof(float)) return fail(ONMT_EINVAL, "bias is not aligned to its elements");
+  if (f8_blocks(M, cols) > kF8MaxBlocks || ((M + 15) / 16) * (int64_t)((rows + 63) / 64) > kF8MaxBlocks)
+    return fail(ONMT_EUNSUPPORTED, "a product of %d x %d by %d rows is too large", M, cols, rows);
+  if (!ws || (uintptr_t)ws % 16) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
+  const size_t need = onmt_f8_linear_ws_bytes(M, cols);
+  if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
+  const Span so = span(out, out_dtype, ld_out, M, rows);
+  if (so.meets(span(x, dtype, ldx, M, cols)) || so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need}) ||
+      so.meets(Span{(uintptr_t)packed, (uintptr_t)packed + onmt_f8_bytes(rows, cols)}))
+    return fail(ONMT_EINVAL, "out overlaps x, ws or packed");
+  hipStream_t st = (hipStream_t)stream;
+  HIP_TRY(f8_linear(x, dtype, ldx, M, f8_mat((void*)packed, rows, cols), rows, cols, bias, out, out_dtype, ld_out, ws, st));
+  return ONMT_OK;
+}
+
+size_t onmt_constrain_ws_bytes(int N, int V, int mode, int K) {
+  if (N < 1 || V < 1 || V > kMaxRuleVocab || mode < 0 || mode > 1 || (mode == 1 && (K < 1 || K > kMaxBeam))) return 0;
+  return constrain_layout(N, V, mode == 1 ? K : 0, nullptr, nullptr);
+}
+
+int onmt_constrain(const onmt_logit_rules* rules, const void* logits, int dtype, int64_t ld, int N, int V, int mode, int K,
+                   void* out, int64_t ld_out, int32_t* ids, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_matrix("logits", logits, dtype, ld, N, V);
+  if (rc) return rc;
+  if (mode < 0 || mode > 2) return fail(ONMT_EINVAL, "mode must be 0 (log-probs), 1 (top-K) or 2 (logits)");
+  if (mode == 1 && (K < 1 || K > kMaxBeam)) return fail(ONMT_EUNSUPPORTED, "K %d outside [1, %d]", K, kMaxBeam);
+  if (mode == 1 && K > V) return fail(ONMT_EINVAL, "K %d larger than the vocabulary", K);
+  if (mode == 1 && !ids) return fail(ONMT_EINVAL, "ids is NULL in top-K mode");
+  if (mode == 2 && lse) return fail(ONMT_EINVAL, "lse must be NULL in mode 2");
+  if (V > kMaxRuleVocab) return fail(ONMT_EUNSUPPORTED, "vocabulary larger than %d", kMaxRuleVocab);
+  if ((V + 4095) / 4096 * (int64_t)N > (1 << 23)) return fail(ONMT_EUNSUPPORTED, "%d rows of %d logits are too many", N, V);
+  const int out_dtype = mode == 2 ? dtype : ONMT_F32;
+  if (mode == 1 && ld_out != K) return fail(ONMT_EINVAL, "ld_out must be K in top-K mode");
+  if ((rc = check_matrix("out", out, out_dtype, ld_out, N, mode == 1 ? K : V))) return rc;
+  const bool same = mode != 1 && out == logits && ld_out == ld && out_dtype == dtype;
+  const Span so = span(out, out_dtype, ld_out, N, mode == 1 ? K : V);
+  if (!same && so.meets(span(logits, dtype, ld, N, V))) return fail(ONMT_EINVAL, "out overlaps the logits");
+  if ((uintptr_t)ids % 4 || (uintptr_t)lse % 4) return fail(ONMT_EINVAL, "ids or lse is not aligned to its elements");
+  LogitRules r{};
+  if (rules && (rc = check_rules(*rules, N, V, &r))) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  const LogitMat m{logits, dtype, ld, N, V};
+  if (mode == 2) {
+    HIP_TRY(rules_logits(r, m, out, ld_out, st));
+    return ONMT_OK;
+  }
+  if (!ws || (uintptr_t)ws % 16) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
+  const size_t need = onmt_constrain_ws_bytes(N, V, mode, K);
+  if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
+  if (so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need})) return fail(ONMT_EINVAL, "out overlaps ws");
+  GenPartials p{};
+  constrain_layout(N, V, mode == 1 ? K : 0, (char*)ws, &p);
+  HIP_TRY(rules_partials(r, m, mode == 1 ? K : 0, (float*)p.pmax, (float*)p.psum, (float*)p.pval, (int32_t*)p.pid, st));
+  if (mode == 0) {
+    HIP_TRY(rules_log_probs(r, m, p.pmax, p.psum, (float*)out, ld_out, lse, st));
+  } else {
+    HIP_TRY(lse_topk_merge(p, N, K, (float*)out, ids, lse, st));
+  }
   return ONMT_OK;
 }
 

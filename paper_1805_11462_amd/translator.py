@@ -130,13 +130,13 @@ class Translator:
         N = B * K
         V = self.cfg.tgt_vocab
         out_state = self.new_state(N)
-        if mode == 0:
+        if mode != 1:               # whole log-probabilities, or (2) the logits, which ops.constrain takes
             logp = torch.empty(N, V, dtype=torch.float32, device=self.device)
             ids = None
         else:
             logp = torch.empty(N, K, dtype=torch.float32, device=self.device)
             ids = torch.empty(N, K, dtype=torch.int32, device=self.device)
-        lse = torch.empty(N, dtype=torch.float32, device=self.device)
+        lse = torch.empty(N, dtype=torch.float32, device=self.device) if mode != 2 else None
         attn = torch.empty(N, S, dtype=torch.float32, device=self.device) if want_attn else None
         n = self.lib.onmt_step_ws_bytes(self.handle, B, S, K)
         ws = _bytes(n, self.device)

@@ -1,0 +1,297 @@
+"""Rules on logits (onmt_constrain) against a plain implementation.
+
+The logits under the rules are defined by fp32 operations that are rounded one by one, so mode 2 and the chosen ids are compared
+exactly with the same operations in NumPy; log-probabilities and logsumexps with 64 bits. Tolerance of those, before any run: a
+row's sum adds its terms in at most 64 steps (16 per lane, 6 across a wave, 16 + 6 over tiles and the exponentials' own
+error), each half a step, 2^-24, of the sum, and the logarithm, the shift and the difference are each within 2^-22 of |lse| and |x|.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1805_11462_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+NO_ID = 0x7FFFFFFF
+
+
+def ruled(x, history=None, history_len=None, repetition=None, presence=None, frequency=None, no_repeat_ngram=0, bias_ids=None,
+          bias=None, mask=None, mask_row=None):
+    """The fp32 logits under the rules, row by row."""
+    x = x.astype(np.float32).copy()
+    N, V = x.shape
+    f32 = np.float32
+    for r in range(N):
+        ban = set()
+        if history is not None:
+            h = [int(t) for t in history[r, :min(max(int(history_len[r]), 0), history.shape[1])]]
+            for v in set(h):
+                if not 0 <= v < V:
+                    continue
+                z = x[r, v]
+                with np.errstate(over="ignore", invalid="ignore"):
+                    if repetition is not None:
+                        z = f32(z / repetition[r]) if z > 0 else f32(z * repetition[r])
+                    if frequency is not None:
+                        z = f32(z - f32(f32(h.count(v)) * frequency[r]))
+                    if presence is not None:
+                        z = f32(z - presence[r])
+                x[r, v] = z
+            n = no_repeat_ngram
+            if n:
+                ban = {h[j] for j in range(n - 1, len(h)) if h[j - n + 1:j] == h[len(h) - n + 1:]}
+        if bias_ids is not None:
+            with np.errstate(over="ignore", invalid="ignore"):
+                for v, b in {int(v): b for v, b in zip(bias_ids[r], bias[r])}.items():
+                    if 0 <= v < V:
+                        x[r, v] = f32(x[r, v] + b)
+        for v in ban:
+            if 0 <= v < V:
+                x[r, v] = -np.inf
+        if mask is not None:
+            t = r if mask_row is None else int(mask_row[r])
+            if t >= 0:
+                v = np.arange(V)
+                on = (mask[t].view(np.uint32)[v >> 5] >> (v & 31).astype(np.uint32)) & 1 if t < mask.shape[0] else np.zeros(V)
+                x[r, on == 0] = -np.inf
+    return x
+
+
+def check(logits, K=5, modes=(0, 1, 2), **rules):
+    """All modes of one call against the plain implementation."""
+    host = {k: (v.cpu().numpy() if isinstance(v, torch.Tensor) else v) for k, v in rules.items()}
+    x = ruled(logits.float().cpu().numpy(), **host)
+    q = ops.LogitRules(**rules) if rules else None
+    if 2 in modes:
+        out, ids, lse = ops.constrain(logits, q, mode=2)
+        assert ids is None and lse is None and out.dtype == logits.dtype
+        want = torch.from_numpy(x).to(logits.dtype)
+        same = (out.cpu() == want) | (out.cpu().isnan() & want.isnan())
+        assert same.all(), torch.nonzero(~same)[:5].tolist()
+    x64 = x.astype(np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        top = x64.max(axis=1, keepdims=True)
+        shift = np.where(np.isfinite(top), top, 0.0)
+        lse64 = shift + np.log(np.exp(x64 - shift).sum(axis=1, keepdims=True))
+        lse64 = np.where(np.isposinf(top) | np.isnan(top), np.nan, lse64)
+        logp64 = np.where(np.isneginf(x64), -np.inf, x64 - lse64)
+        tol = 64 * 2.0 ** -24 + 2.0 ** -22 * (np.abs(lse64) + np.abs(np.where(np.isneginf(x64), 0.0, x64)))
+
+    def near(got, want, t):
+        got = got.double().cpu().numpy()
+        special = ~np.isfinite(want)
+        assert np.array_equal(got[special], want[special], equal_nan=True)
+        err = np.abs(got[~special] - want[~special])
+        assert (err <= np.broadcast_to(t, want.shape)[~special]).all(), err.max()
+
+    if 0 in modes:
+        out, ids, lse = ops.constrain(logits, q, mode=0)
+        assert ids is None
+        near(lse[:, None], lse64, np.where(np.isfinite(lse64), tol.max(axis=1, keepdims=True), 0.0))
+        near(out, logp64, tol)
+    if 1 in modes:
+        K = min(K, logits.shape[1])
+        out, ids, lse = ops.constrain(logits, q, mode=1, K=K)
+        rank = np.where(np.isnan(x), -np.inf, x)
+        order = np.argsort(-rank, axis=1, kind="stable")[:, :K]
+        some = np.take_along_axis(rank, order, 1) > -np.inf
+        assert np.array_equal(ids.cpu().numpy(), np.where(some, order, NO_ID))
+        with np.errstate(invalid="ignore"):
+            near(out, np.where(some, np.take_along_axis(logp64, order, 1), -np.inf), np.take_along_axis(tol, order, 1))
+        near(lse[:, None], lse64, np.where(np.isfinite(lse64), tol.max(axis=1, keepdims=True), 0.0))
+
+
+def everything(N, V, T=40, nbias=6, tables=3, seed=0, ngram=2):
+    """Rules of every kind: ids drawn from few, some outside the vocabulary, lists with repeated ids, lengths out of range."""
+    g = np.random.default_rng(seed)
+    pool = g.integers(0, V, 12)
+    h = pool[g.integers(0, 12, (N, T))]
+    h[g.random((N, T)) < 0.05] = -1
+    h[g.random((N, T)) < 0.05] = V
+    n = g.integers(0, T + 1, N)
+    n[0] = T
+    if N > 2:
+        n[1], n[2] = -3, T + 100
+    ids = g.integers(-1, V + 1, (N, nbias))
+    ids[:, -1] = ids[:, 0]
+    words = (V + 31) // 32
+    mask = g.integers(0, 1 << 32, (tables, words), dtype=np.uint64).astype(np.uint32)
+    row = g.integers(-1, tables, N)
+    c = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    return dict(history=c(h.astype(np.int32)), history_len=c(n.astype(np.int32)),
+                repetition=c((1 + g.random(N)).astype(np.float32)), presence=c(g.random(N).astype(np.float32)),
+                frequency=c(g.standard_normal(N).astype(np.float32)), no_repeat_ngram=ngram,
+                bias_ids=c(ids.astype(np.int32)), bias=c((4 * g.standard_normal((N, nbias))).astype(np.float32)),
+                mask=c(mask.view(np.int32)), mask_row=c(row.astype(np.int32)))
+
+
+def logits_of(N, V, kind, seed=1):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (3 * torch.randn(N, V, generator=g, device="cuda")).to(TYPES[kind])
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("V", [1, 3, 31, 33, 64, 1000, 1024, 1025, 4096, 4099, 9001, 50001, 131072])
+def test_vocabularies(V, kind):
+    print(f"[case] V {V} {kind}", flush=True)
+    x = logits_of(5, V, kind)
+    check(x, K=16)
+    check(x, K=5, **everything(5, V))
+
+
+@pytest.mark.parametrize("K", [1, 2, 5, 8, 16])
+def test_widths(K):
+    for kind in ("f32", "bf16"):
+        check(logits_of(9, 6000, kind, seed=K), K=K, modes=(1,), **everything(9, 6000, seed=K))
+
+
+@pytest.mark.parametrize("ngram", [1, 2, 3, 5, 60])
+def test_ngrams(ngram):
+    for T in (1, 2, 5, 50):
+        rules = everything(6, 40, T=T, ngram=ngram, seed=ngram)
+        check(logits_of(6, 40, "f32"), **{k: rules[k] for k in ("history", "history_len", "no_repeat_ngram")})
+
+
+@pytest.mark.parametrize("names", [("history", "history_len", "repetition"), ("history", "history_len", "presence"),
+                                   ("history", "history_len", "frequency"), ("bias_ids", "bias"), ("mask", "mask_row"),
+                                   ("history", "history_len"), ("history", "history_len", "bias_ids", "bias"),
+                                   ("bias_ids", "bias", "mask", "mask_row")])
+def test_each_rule_alone(names):
+    rules = everything(7, 5000)
+    check(logits_of(7, 5000, "f32"), **{k: rules[k] for k in names})
+
+
+def test_a_long_history_and_long_lists():
+    check(logits_of(3, 9000, "f32"), **everything(3, 9000, T=3000, nbias=2000, ngram=3))
+
+
+def test_a_table_per_row_and_none():
+    rules = everything(6, 300, tables=6)
+    x = logits_of(6, 300, "f16")
+    check(x, mask=rules["mask"])
+    # a table past the last forbids every token
+    row = torch.tensor([0, 5, 6, 1000000, -1, -2**31], dtype=torch.int32, device="cuda")
+    check(x, mask=rules["mask"], mask_row=row)
+
+
+def test_rows_without_a_token_and_with_few():
+    V = 2500
+    x = logits_of(4, V, "f32")
+    bits = np.zeros((4, (V + 31) // 32), np.uint32)
+    bits[1, 70] = 1 << 5                       # one token
+    bits[2, ::7] = 1 << 31                     # a dozen
+    bits[3, -1] = 1 << 3                       # V - 1 = 2499 = 78 * 32 + 3
+    check(x, K=16, mask=torch.from_numpy(bits.view(np.int32)).cuda())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_ties_zeros_and_special_values(kind):
+    V = 6000
+    t = TYPES[kind]
+    x = torch.zeros(8, V, device="cuda", dtype=t)
+    x[1] = -0.0
+    x[1, 1::2] = 0.0
+    x[2] = torch.finfo(t).min
+    x[3] = float("-inf")
+    x[4, 100] = float("nan")
+    x[5, 200] = float("inf")
+    x[6] = torch.finfo(t).max
+    x[7, ::3] = 1.0                            # 2000 equal largest ones
+    check(x, K=16)
+    # under a mask none of it shows
+    keep = np.full((1, (V + 31) // 32), 0xFFFFFFFF, np.uint32)
+    keep[0, 100 // 32] = keep[0, 200 // 32] = 0
+    check(x, K=3, mask=torch.from_numpy(keep.view(np.int32)).cuda(), mask_row=torch.zeros(8, dtype=torch.int32, device="cuda"))
+
+
+def test_strides_odd_addresses_and_in_place():
+    for kind in TYPES:
+        N, V = 6, 4501
+        base = logits_of(N, V + 11, kind)
+        x = base[:, 5:5 + V]
+        rules = everything(N, V)
+        check(x, **rules)
+        q = ops.LogitRules(**rules)
+        want = ops.constrain(x, q, mode=2)[0]
+        logp = ops.constrain(x, q, mode=0)[0]
+        keep = base.clone()
+        wide = torch.full((N, V + 4), 9.0, device="cuda")
+        ops.constrain(x, q, mode=0, out=wide[:, 1:1 + V])
+        assert torch.equal(wide[:, 1:1 + V], logp) and (wide[:, 0] == 9).all() and (wide[:, 1 + V:] == 9).all()
+        if kind == "f32":
+            y = base.clone()[:, 5:5 + V]
+            assert ops.constrain(y, q, mode=0, out=y)[0] is y
+            assert torch.equal(y, logp)
+        assert ops.constrain(x, q, mode=2, out=x)[0] is x
+        assert torch.equal(x, want)
+        assert torch.equal(base[:, :5], keep[:, :5]) and torch.equal(base[:, 5 + V:], keep[:, 5 + V:])
+
+
+def test_offsets_past_32_bits():
+    N, V = 17000, 131072                      # 2.2e9 logits
+    x = torch.zeros(N, V, dtype=torch.bfloat16, device="cuda")
+    for r in (0, 16383, 16384, N - 1):
+        x[r] = logits_of(1, V, "bf16", seed=r)[0]
+    out, ids, lse = ops.constrain(x, None, mode=1, K=4)
+    y = ops.constrain(x, None, mode=2)[0]
+    for r in (0, 16383, 16384, N - 1):
+        o2, i2, l2 = ops.constrain(x[r:r + 1].clone(), None, mode=1, K=4)
+        assert torch.equal(out[r:r + 1], o2) and torch.equal(ids[r:r + 1], i2) and torch.equal(lse[r:r + 1], l2)
+        assert torch.equal(y[r], x[r])
+    assert torch.equal(ids[5].cpu(), torch.arange(4, dtype=torch.int32))
+
+
+def test_other_streams_and_captured():
+    N, V = 40, 20000
+    x = logits_of(N, V, "f32")
+    q = ops.LogitRules(**everything(N, V))
+    want = [ops.constrain(x, q, mode=m, K=5)[0] for m in range(3)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        got = []
+        for m, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got.append(ops.constrain(x, q, mode=m, K=5)[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for mode in range(3):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = ops.constrain(x, q, mode=mode, K=5)
+        for seed in range(3):
+            x.copy_(logits_of(N, V, "f32", seed=30 + seed))
+            graph.replay()
+            for a, b in zip(got, ops.constrain(x, q, mode=mode, K=5)):
+                assert a is b is None or torch.equal(a, b)
+            torch.cuda.synchronize()
+
+
+def test_refused_tensors():
+    r = everything(4, 100)
+    x = logits_of(4, 100, "f32")
+    q = ops.LogitRules(**r)
+    for bad in (x[:3], x.cpu(), x.double(), x.t(), x[0], x[:, ::2]):
+        with pytest.raises(ValueError):
+            ops.constrain(bad, q)
+    with pytest.raises(ValueError):
+        ops.constrain(logits_of(4, 129, "f32"), q)               # the mask covers 128 tokens
+    with pytest.raises(ValueError):
+        ops.constrain(x, q, mode=3)
+    with pytest.raises(ValueError):
+        ops.constrain(x, q, mode=0, out=x.bfloat16())
+    for kw in (dict(history=r["history"]), dict(bias=r["bias"]), dict(mask_row=r["mask_row"]),
+               dict(history=r["history"], history_len=r["history_len"][:3]),
+               dict(history=r["history"].long(), history_len=r["history_len"]),
+               dict(history=r["history"], history_len=r["history_len"], repetition=r["repetition"].double()),
+               dict(bias_ids=r["bias_ids"], bias=r["bias"][:, :2]), dict(mask=r["mask"].long()),
+               dict(mask=r["mask"].cpu())):
+        with pytest.raises(ValueError):
+            ops.LogitRules(**kw)
