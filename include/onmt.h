@@ -304,8 +304,9 @@ int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* pac
  *   no_repeat_ngram = n > 0 and the history holds the n-gram (its last n - 1 ids, v):  x = -inf
  *   mask bit v & 31 of word v >> 5 is 0:  x = -inf, whatever it was (NaN too)
  * All pointers are device pointers; a NULL one switches its rule off (without a history nothing is repeated). history [N, max_history] (row stride history_stride) holds
- * history_len[r] ids of row r (clamped to [0, max_history]); what lies behind is not read. Ids outside [0, V) in histories and
+ * history_len[r] ids of row r (clamped to [0, max_history]; what lies behind does not matter). Ids outside [0, V) in histories and
  * bias lists match no token (in n-grams they are ids like others). bias_ids, bias: [N, n_bias], row stride bias_stride.
+ * max_history and n_bias are at most 65535 (ONMT_EUNSUPPORTED beyond).
  * mask: n_masks tables of ceil(V / 32) words (row stride mask_stride); row r uses table mask_row[r] (any negative number: none;
  * n_masks or more: every token is forbidden), or table r where mask_row is NULL (n_masks >= N). */
 typedef struct {

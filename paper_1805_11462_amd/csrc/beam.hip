@@ -44,14 +44,14 @@ __device__ __forceinline__ void row_tiles_load(const float* __restrict__ pmax, c
   }
 }
 
-// The row's logsumexp, in every lane (-inf for a row without a candidate).
+// The row's logsumexp, in every lane.
 __device__ __forceinline__ float row_lse(const float (&tm)[kMaxTilesPerLane], const float (&tq)[kMaxTilesPerLane],
                                          int ntiles) {
   const int lane = threadIdx.x & 63;
   float mx = -__builtin_inff();
 #pragma unroll
   for (int j = 0; j < kMaxTilesPerLane; ++j) mx = fmaxf(mx, tm[j]);
-  const float top = wave_max(mx), gmx = top > -__builtin_inff() ? top : 0.f;
+  const float gmx = wave_max(mx);
   float sm = 0.f;
 #pragma unroll
   for (int j = 0; j < kMaxTilesPerLane; ++j) {

@@ -318,16 +318,16 @@ struct LogitMat {
   int64_t ld;
   int N, V;
 };
-// Columns per entry of the partials and lists that the first pass leaves: pmax, psum [N, tiles], pval, pid [N, tiles, K].
-constexpr int kRuleTile = 1024;
 // out [N, V] in the logits' own type.
 hipError_t rules_logits(const LogitRules& r, const LogitMat& m, void* out, int64_t ld_out, hipStream_t st);
-// Partials; with K > 0 also each tile's top-K list.
-hipError_t rules_partials(const LogitRules& r, const LogitMat& m, int K, float* pmax, float* psum, float* pval, int32_t* pid,
-                          hipStream_t st);
-// logp [N, V] from the logits again and the rows' partials; lse optional.
-hipError_t rules_log_probs(const LogitRules& r, const LogitMat& m, const float* pmax, const float* psum, float* logp,
-                           int64_t ld_out, float* lse, hipStream_t st);
+// Scratch of the calls below (K = 0: log-probabilities).
+size_t rules_ws(int N, int V, int K);
+// out, ids [N, K] = the K largest log-probabilities; lse optional.
+hipError_t rules_top(const LogitRules& r, const LogitMat& m, int K, void* ws, float* out, int32_t* ids, float* lse,
+                     hipStream_t st);
+// logp [N, V]; lse optional.
+hipError_t rules_log_probs(const LogitRules& r, const LogitMat& m, void* ws, float* logp, int64_t ld_out, float* lse,
+                           hipStream_t st);
 
 hipError_t fill_f32(float* dst, size_t n, float v, hipStream_t st);
 // Zeros in columns width .. 32 kblocks of every row (rows rounded up to whole blocks) of up to two two-term operands.

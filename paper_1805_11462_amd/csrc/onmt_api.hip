@@ -1252,7 +1252,7 @@ int check_beam(const onmt_model* m, int S, int K) {
 
 // ------------------------------------------------------------------ matrices of a caller's type, rules on logits
 constexpr int64_t kF8MaxBlocks = 1 << 24;
-constexpr int kMaxRuleVocab = 1 << 20;
+constexpr int kMaxRuleVocab = 1 << 20, kMaxRuleList = 65535;      // lists: counts and entries share a word
 
 int64_t f8_blocks(int64_t rows, int64_t cols) { return ((rows + 15) / 16) * ((cols + kF8Block - 1) / kF8Block); }
 size_t elem_bytes(int dtype) { return dtype == ONMT_F32 ? 4 : 2; }
@@ -1296,32 +1296,14 @@ int check_rules(const onmt_logit_rules& q, int N, int V, LogitRules* r) {
     return fail(ONMT_EINVAL, "a bias list needs bias_ids, bias and bias_stride >= n_bias");
   if (q.mask && (q.n_masks < 1 || q.mask_stride < (V + 31) / 32 || (!q.mask_row && q.n_masks < N)))
     return fail(ONMT_EINVAL, "masks need mask_stride >= ceil(V / 32) and n_masks >= 1 (>= N without mask_row)");
+  if (q.history && q.max_history > kMaxRuleList) return fail(ONMT_EUNSUPPORTED, "max_history larger than %d", kMaxRuleList);
+  if (q.n_bias > kMaxRuleList) return fail(ONMT_EUNSUPPORTED, "n_bias larger than %d", kMaxRuleList);
   const void* words[] = {q.history, q.history_len, q.repetition, q.presence, q.frequency, q.bias_ids, q.bias, q.mask, q.mask_row};
   for (const void* p : words)
     if ((uintptr_t)p % 4) return fail(ONMT_EINVAL, "an array of the rules is not aligned to its elements");
   *r = LogitRules{q.history, q.history_len, q.history_stride, q.max_history, q.repetition, q.presence, q.frequency, q.no_repeat_ngram,
                   q.bias_ids, q.bias, q.bias_stride, q.n_bias, q.mask, q.mask_stride, q.n_masks, q.mask_row};
   return ONMT_OK;
-}
-
-size_t constrain_layout(int N, int V, int K, char* base, GenPartials* p) {
-  Carver c;
-  c.base = base;
-  const int nt = (V + kRuleTile - 1) / kRuleTile;
-  const size_t n = (size_t)N * nt;
-  float* pmax = c.take<float>(n);
-  float* psum = c.take<float>(n);
-  float* pval = K > 0 ? c.take<float>(n * K) : nullptr;
-  int32_t* pid = K > 0 ? c.take<int32_t>(n * K) : nullptr;
-  if (p) {
-    p->pmax = pmax;
-    p->psum = psum;
-    p->pval = pval;
-    p->pid = pid;
-    p->ntiles = nt;
-    p->V = V;
-  }
-  return c.off;
 }
 
 }  // namespace
@@ -1751,7 +1733,7 @@ int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* pac
 
 size_t onmt_constrain_ws_bytes(int N, int V, int mode, int K) {
   if (N < 1 || V < 1 || V > kMaxRuleVocab || mode < 0 || mode > 1 || (mode == 1 && (K < 1 || K > kMaxBeam))) return 0;
-  return constrain_layout(N, V, mode == 1 ? K : 0, nullptr, nullptr);
+  return rules_ws(N, V, mode == 1 ? K : 0);
 }
 
 int onmt_constrain(const onmt_logit_rules* rules, const void* logits, int dtype, int64_t ld, int N, int V, int mode, int K,
@@ -1784,14 +1766,8 @@ int onmt_constrain(const onmt_logit_rules* rules, const void* logits, int dtype,
   const size_t need = onmt_constrain_ws_bytes(N, V, mode, K);
   if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   if (so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need})) return fail(ONMT_EINVAL, "out overlaps ws");
-  GenPartials p{};
-  constrain_layout(N, V, mode == 1 ? K : 0, (char*)ws, &p);
-  HIP_TRY(rules_partials(r, m, mode == 1 ? K : 0, (float*)p.pmax, (float*)p.psum, (float*)p.pval, (int32_t*)p.pid, st));
-  if (mode == 0) {
-    HIP_TRY(rules_log_probs(r, m, p.pmax, p.psum, (float*)out, ld_out, lse, st));
-  } else {
-    HIP_TRY(lse_topk_merge(p, N, K, (float*)out, ids, lse, st));
-  }
+  HIP_TRY(mode == 0 ? rules_log_probs(r, m, ws, (float*)out, ld_out, lse, st)
+                    : rules_top(r, m, K, ws, (float*)out, ids, lse, st));
   return ONMT_OK;
 }
 

@@ -6,10 +6,16 @@
 // is 0, gets -inf whatever it was.
 //
 // A workgroup takes 4096 consecutive tokens of a row and every wave 1024 of them, 16 per lane, in 16-byte accesses. The rules
-// name tokens, not places: occurrences are counted in LDS, one word per token of the slice (integer atomics, so their
-// order does not matter; the top bit marks an n-gram's end), and of a bias list each token keeps its last entry's index (atomic
-// maximum). The logits are loaded before that and wait in registers. What bounds it is memory: each logit is read once
-// (twice for whole log-probabilities, the second time from the caches where the batch fits them) and each output written once.
+// name tokens, not places, and few of them: the occurrences of a history's tokens in the slice are counted in LDS (integer
+// atomics, so their order does not matter), the first to touch a token lists it, and one thread per listed token then forms
+// its new logit, which the lane that holds the token fetches where a bitmap says so. Bias lists go the same way with an atomic
+// maximum of entry indices. (Every lane looking up a count for each of its 16 tokens, divisions and all, took
+// 322 us at 2560 x 50000 bf16 where memory alone takes 50.) The logits are loaded before that and wait in registers. What
+// bounds it is memory: each logit is read once (twice for whole log-probabilities, the second time from the caches where the
+// batch fits them) and each output written once.
+
+#include <cstddef>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -17,125 +23,224 @@
 
 namespace onmt {
 
-constexpr int kSlice = 4096, kThreads = 256, kPerLane = 16;
-static_assert(kSlice == kThreads * kPerLane && kRuleTile == kWave * kPerLane, "a wave's tokens are a tile");
+constexpr int kThreads = 256;
 constexpr int kNoId = 0x7fffffff;
-constexpr uint32_t kEnds = 0x80000000u;        // top bit of a count: the token would end a repeated n-gram
-
-// The lane's tokens: position i of vector u (kVec<T> tokens each) is base + u * (64 kVec<T>) + i.
-template <class T>
+// The lane's PER tokens: position i of vector u (VEC tokens each) is base + u * (64 VEC) + i. A wave's tokens are a tile, a
+// workgroup's a slice.
+template <int PER_, int VEC_>
 struct Tokens {
-  static constexpr int VEC = kVec<T>, NV = kPerLane / VEC;
+  static constexpr int PER = PER_, VEC = VEC_, NV = PER / VEC, TILE = PER * kWave, SLICE = PER * kThreads;
   int slice0, base;
   __device__ __forceinline__ explicit Tokens(int slice)
-      : slice0(slice * kSlice), base(slice0 + (threadIdx.x >> 6) * kRuleTile + (threadIdx.x & 63) * VEC) {}
+      : slice0(slice * SLICE), base(slice0 + (threadIdx.x >> 6) * TILE + (threadIdx.x & 63) * VEC) {}
   __device__ __forceinline__ int at(int u) const { return base + u * kWave * VEC; }
 };
 
-// One token's penalties and bias, every operation rounded by itself.
+template <class T, int VEC>
+__device__ __forceinline__ void load_some(const T* p, float* v) {
+  typedef T vec __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+  const vec x = *(const vec*)p;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = (float)x[i];
+}
+
+// One token's penalties, every operation rounded by itself.
 __device__ __forceinline__ float penalized(float z, float times, bool rep, float rho, float freq, float pres) {
 #pragma clang fp contract(off)
   if (rep) z = z > 0.f ? z / rho : z * rho;
   return (z - times * freq) - pres;
 }
 
-// v = the lane's logits of row `row` under the rules, -inf past V. lds: 4096 words of counts (with a history), then 4096 of
-// bias entries (with biases).
-template <class T>
-__device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, int row, const Tokens<T>& tk,
-                                      uint32_t* lds, float (&v)[kPerLane]) {
-  constexpr int VEC = Tokens<T>::VEC, NV = Tokens<T>::NV;
+// The largest value of a row of 16 lanes that holds the same in every row, in every lane.
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, dpp_move<0x111, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x112, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x114, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x118, 0xf>(v, v));
+  return readlane_f(v, 15);
+}
+
+// Takes the lanes that hold `theta` out of c; how many they were.
+__device__ __forceinline__ int taken(float& c, float theta) {
+  const bool is = c == theta;
+  c = is ? -__builtin_inff() : c;
+  return __popcll(__ballot(is));
+}
+
+// Workgroup barrier for what lies in LDS only: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Per token of the slice a word (occurrences in the low half, last bias entry + 1 in the high half; then the new logit); the
+// touched tokens as bits and, up to LIST of them, as a list (more: every token's bit is looked at); the tokens that would
+// end a repeated n-gram. Small enough for eight workgroups per CU, which hide each other's trips to memory.
+template <int PER>
+struct RuleLds {
+  static constexpr int SLICE = PER * kThreads, WORDS = SLICE / 32;
+  static constexpr int LIST = 1024;
+  uint32_t word[SLICE];
+  uint16_t list[LIST];
+  uint32_t touched[WORDS];
+  uint32_t ends[WORDS];
+  int n;
+};
+
+template <class S>
+__device__ __forceinline__ void touch(S& s, int o) {
+  const uint32_t bit = 1u << (o & 31);
+  if (atomicOr(&s.touched[o >> 5], bit) & bit) return;
+  const int at = atomicAdd(&s.n, 1);
+  if (at < s.LIST) s.list[at] = (uint16_t)o;
+}
+
+// v = the lane's logits of row `row` under the rules, -inf past V. s: used where there is a history or a bias list. Everything
+// whose address is known at the start is loaded there (the first entries of the lists too), so that one trip to memory is
+// exposed instead of one per rule (2560 x 50000 bf16 with every rule: 236 us before).
+// LISTS: there is a history or a bias list.
+template <class T, bool LISTS, int PER, int VEC>
+__device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, int row, const Tokens<PER, VEC>& tk,
+                                      RuleLds<PER>& s, float (&v)[PER]) {
+  constexpr int NV = Tokens<PER, VEC>::NV, SLICE = Tokens<PER, VEC>::SLICE;
   const float ninf = -__builtin_inff();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, width = min(SLICE, V - tk.slice0);
+  const bool penalties = LISTS && q.history && (q.repetition || q.presence || q.frequency);
+  const bool ngrams = LISTS && q.history && q.ngram > 0;
+  const int32_t* h = q.history + (int64_t)row * q.history_stride;
+  const int32_t* ids = q.bias_ids + (int64_t)row * q.bias_stride;
+  const int n = LISTS && q.history ? min(max(q.history_len[row], 0), q.max_history) : 0, g = q.ngram;
+  const int mr = q.mask ? (q.mask_row ? q.mask_row[row] : row) : -1;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     const int t = tk.at(u);
     if (t + VEC <= V) {
-      load_vec(x + t, &v[u * VEC]);
+      load_some<T, VEC>(x + t, &v[u * VEC]);
     } else {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) v[u * VEC + i] = t + i < V ? to_float(x[t + i]) : ninf;
     }
   }
-  uint32_t* cnt = lds;
-  int* which = (int*)(lds + (q.history ? kSlice : 0));
-  if (q.history || q.n_bias) {
-    if (q.history)
-      for (int i = tid; i < kSlice / 4; i += kThreads) ((uint4*)cnt)[i] = make_uint4(0, 0, 0, 0);
-    if (q.n_bias)
-      for (int i = tid; i < kSlice / 4; i += kThreads) ((int4*)which)[i] = make_int4(-1, -1, -1, -1);
-    __syncthreads();
-    const int width = min(kSlice, V - tk.slice0);
-    if (q.history) {
-      const int32_t* h = q.history + (int64_t)row * q.history_stride;
-      const int n = min(max(q.history_len[row], 0), q.max_history);
-      const int g = q.ngram;
-      for (int j = tid; j < n; j += kThreads) {
-        const int id = h[j], o = id - tk.slice0;
-        if (id < tk.slice0 || o >= width) continue;
-        atomicAdd(&cnt[o], 1u);
-        if (g > 0 && j >= g - 1) {
-          bool same = true;
-          for (int i = 1; i < g && same; ++i) same = h[j - i] == h[n - i];
-          if (same) atomicOr(&cnt[o], kEnds);
-        }
-      }
-    }
-    if (q.n_bias) {
-      const int32_t* ids = q.bias_ids + (int64_t)row * q.bias_stride;
-      for (int j = tid; j < q.n_bias; j += kThreads) {
-        const int id = ids[j], o = id - tk.slice0;
-        if (id >= tk.slice0 && o < width) atomicMax(&which[o], j);
-      }
-    }
-    __syncthreads();
-    const float rho = q.repetition ? q.repetition[row] : 1.f;
-    const float pres = q.presence ? q.presence[row] : 0.f;
-    const float freq = q.frequency ? q.frequency[row] : 0.f;
-    const float* bias = q.n_bias ? q.bias + (int64_t)row * q.bias_stride : nullptr;
-#pragma unroll
-    for (int u = 0; u < NV; ++u)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int o = tk.at(u) - tk.slice0 + i;
-        float z = v[u * VEC + i];
-        if (q.history) {
-          const uint32_t c = cnt[o];
-          if (c) {
-            z = penalized(z, (float)(c & ~kEnds), q.repetition != nullptr, rho, freq, pres);
-          }
-          if (q.n_bias && which[o] >= 0) z = z + bias[which[o]];
-          if (c & kEnds) z = ninf;
-        } else if (which[o] >= 0) {
-          z = z + bias[which[o]];
-        }
-        v[u * VEC + i] = tk.at(u) + i < V ? z : ninf;
-      }
+  int hid = -1, prev = 0, bid = -1;
+  if constexpr (LISTS) {
+    if (q.history && tid < q.max_history) hid = h[tid];
+    if (ngrams && g > 1 && tid > 0 && tid < q.max_history) prev = h[tid - 1];
+    if (tid < q.n_bias) bid = ids[tid];
   }
-  if (q.mask) {
-    const int mr = q.mask_row ? q.mask_row[row] : row;
-    if (mr >= 0) {
-      const uint32_t* bits = q.mask + (int64_t)min(mr, q.n_masks - 1) * q.mask_stride;
+  uint32_t on[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int t = tk.at(u);
+    on[u] = ~0u;
+    if (mr >= 0) on[u] = t < V && mr < q.n_masks ? q.mask[(int64_t)mr * q.mask_stride + (t >> 5)] >> (t & 31) : 0u;
+  }
+  // the bits of vector u's tokens
+  auto bits_of = [&](const uint32_t* b, int u) {
+    const int o = tk.at(u) - tk.slice0;
+    return b[o >> 5] >> (o & 31) & ((1u << VEC) - 1);
+  };
+  if constexpr (LISTS) {
+#pragma unroll
+    for (int i = 0; i < PER / 4; ++i) ((uint4*)s.word)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
+    if (tid < s.WORDS) s.touched[tid] = s.ends[tid] = 0;
+    if (tid == 0) s.n = 0;
+    lds_barrier();
+    if (q.n_bias) {
+      auto entry = [&](int id, int j) {
+        const int o = id - tk.slice0;
+        if (id < tk.slice0 || o >= width || j >= q.n_bias) return;
+        atomicMax(&s.word[o], (uint32_t)(j + 1) << 16);
+        touch(s, o);
+      };
+      entry(bid, tid);
+      for (int j = tid + kThreads; j < q.n_bias; j += kThreads) entry(ids[j], j);
+      lds_barrier();
+    }
+    if (q.history) {
+      const int last = n > 0 ? h[n - 1] : 0;
+      auto entry = [&](int id, int before_it, int j) {
+        const int o = id - tk.slice0;
+        if (id < tk.slice0 || o >= width || j >= n) return;
+        if (penalties) {
+          atomicAdd(&s.word[o], 1u);
+          touch(s, o);
+        }
+        if (ngrams && j >= g - 1 && (g == 1 || before_it == last)) {
+          bool same = true;
+          for (int i = 2; i < g && same; ++i) same = h[j - i] == h[n - i];
+          if (same) atomicOr(&s.ends[o >> 5], 1u << (o & 31));
+        }
+      };
+      entry(hid, prev, tid);
+      for (int j0 = kThreads; j0 < n; j0 += 4 * kThreads) {      // four loads in flight
+        int id[4], before_it[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int j = j0 + tid + a * kThreads;
+          id[a] = j < n ? h[j] : -1;
+          before_it[a] = ngrams && g > 1 && j < n ? h[j - 1] : 0;
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) entry(id[a], before_it[a], j0 + tid + a * kThreads);
+      }
+      lds_barrier();
+    }
+    if (penalties || q.n_bias) {
+      const float rho = penalties && q.repetition ? q.repetition[row] : 1.f;
+      const float pres = penalties && q.presence ? q.presence[row] : 0.f;
+      const float freq = penalties && q.frequency ? q.frequency[row] : 0.f;
+      const float* bias = q.bias + (int64_t)row * q.bias_stride;
+      const bool listed = s.n <= s.LIST;
+      for (int i = tid; i < (listed ? s.n : SLICE); i += kThreads) {
+        const int o = listed ? s.list[i] : i;
+        if (!listed && !(s.touched[o >> 5] >> (o & 31) & 1)) continue;
+        const uint32_t w = s.word[o], c = w & 0xffff, j = w >> 16;
+        float z = to_float(x[tk.slice0 + o]);
+        const float b = j ? bias[j - 1] : 0.f;
+        if (c) z = penalized(z, (float)c, q.repetition != nullptr, rho, freq, pres);
+        if (j) z += b;
+        s.word[o] = __builtin_bit_cast(uint32_t, z);
+      }
+      lds_barrier();
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int t = tk.at(u);
-        const uint32_t word = t < V && mr < q.n_masks ? bits[t >> 5] >> (t & 31) : 0u;
+        const uint32_t b = bits_of(s.touched, u);
+        if (b) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (!((word >> i) & 1u)) v[u * VEC + i] = ninf;
+          for (int i = 0; i < VEC; i += 4) {
+            const uint4 w = *(const uint4*)&s.word[tk.at(u) - tk.slice0 + i];
+            v[u * VEC + i] = b >> i & 1 ? __builtin_bit_cast(float, w.x) : v[u * VEC + i];
+            v[u * VEC + i + 1] = b >> i & 2 ? __builtin_bit_cast(float, w.y) : v[u * VEC + i + 1];
+            v[u * VEC + i + 2] = b >> i & 4 ? __builtin_bit_cast(float, w.z) : v[u * VEC + i + 2];
+            v[u * VEC + i + 3] = b >> i & 8 ? __builtin_bit_cast(float, w.w) : v[u * VEC + i + 3];
+          }
+        }
+      }
+    }
+  }
+  // what is forbidden, -inf: x = (x & keep) | (-inf & ~keep) with each bit spread over a word
+  if (ngrams || mr >= 0) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const uint32_t b = ngrams ? on[u] & ~bits_of(s.ends, u) : on[u];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const uint32_t keep = (uint32_t)((int)(b << (31 - i)) >> 31);
+        v[u * VEC + i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v[u * VEC + i]) & keep) | (0xff800000u & ~keep));
       }
     }
   }
 }
 
-template <class T>
+template <class T, int PER, bool LISTS>
 __global__ __launch_bounds__(kThreads) void k_rules_logits(LogitRules q, const T* x, int64_t ld, int V, int slices,
                                                            T* out, int64_t ld_out) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   const int row = blockIdx.x / slices;
-  const Tokens<T> tk(blockIdx.x % slices);
-  float v[kPerLane];
-  ruled(q, x + (int64_t)row * ld, V, row, tk, lds, v);
+  const Tokens<PER, kVec<T>> tk(blockIdx.x % slices);
+  float v[PER];
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
   T* o = out + (int64_t)row * ld_out;
 #pragma unroll
   for (int u = 0; u < tk.NV; ++u) {
@@ -150,91 +255,81 @@ __global__ __launch_bounds__(kThreads) void k_rules_logits(LogitRules q, const T
   }
 }
 
-// Rows' partials: a tile's largest value and the sum of exp(v - that) (NaN where one is; a +inf makes it NaN too). K > 0: the
-// tile's top K, larger first, smaller id on ties, by one wave: theta, the K-th largest of the lanes' maxima, is at most the tile's
-// K-th largest value, found bit by bit with ballots; the values that reach it, K or a few more, are ranked against
-// each other, one per lane. Tiles with more of them than lanes (ties) take K rounds of an argmax.
-template <class T, bool LISTS>
+// What the first pass leaves of each tile of a row: largest value and sum of exp, and (K > 0) a list of the candidates for the
+// row's K largest, as (value, id).
+struct RulePartials {
+  uint2* list;
+  float* max;                   // [N, ntiles]
+  float* sum;
+  int* count;
+  int ntiles, K;
+};
+
+// Entries of a tile's list: as many values as may pass its bound, or the K largest.
+__host__ __device__ inline int list_cap(int K) { return 4 * K < 32 ? 4 * K : 32; }
+
+// Rows' partials: a tile's largest value and the sum of exp(v - that) (NaN where one is; a +inf makes it NaN too). TOP: the
+// values that can be among the row's K largest, at most list_cap(K) of each tile. theta, the K-th largest of the maxima of
+// 16 groups of four lanes (K > 8: of the 64 lanes), is at most the tile's K-th largest value: those that reach it, K or a few
+// more, are listed in no order. Tiles with more of them (ties) list the K largest, by K rounds of an argmax. Ranking belongs
+// to the row's merge. (2560 x 50000 bf16 at K = 5: theta bit by bit with ballots and lists ranked here took 331 scalar
+// and 357 vector instructions per wave, and either unit was as long in it as the memory.)
+template <class T, int PER, bool LISTS, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const T* __restrict__ x, int64_t ld, int V, int slices,
-                                                             int ntiles, int K, float* __restrict__ pmax,
-                                                             float* __restrict__ psum, float* __restrict__ pval,
-                                                             int32_t* __restrict__ pid) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-  __shared__ float sv[kThreads / kWave][kWave];
-  __shared__ int si[kThreads / kWave][kWave];
+                                                             RulePartials p) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
-  const Tokens<T> tk(slice);
-  constexpr int VEC = Tokens<T>::VEC;
+  constexpr int VEC = kVec<T>;
+  const Tokens<PER, VEC> tk(slice);
   const float ninf = -__builtin_inff();
-  float v[kPerLane];
-  ruled(q, x + (int64_t)row * ld, V, row, tk, lds, v);
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int tile = slice * (kSlice / kRuleTile) + w;
-  if (tile >= ntiles) return;
+  float v[PER];
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
+  const int lane = threadIdx.x & 63;
+  const int tile = slice * (kThreads / kWave) + (threadIdx.x >> 6);
+  if (tile >= p.ntiles) return;
   float m = ninf;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) m = fmaxf(m, v[i]);
+  for (int i = 0; i < PER; ++i) m = fmaxf(m, v[i]);
   const float top = wave_max(m), shift = top > ninf ? top : 0.f;
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) s += __expf(v[i] - shift);
+  for (int i = 0; i < PER; ++i) s += __expf(v[i] - shift);
   s = wave_sum(s);
-  const size_t o = (size_t)row * ntiles + tile;
-  if (lane == 0) {
-    pmax[o] = top;
-    psum[o] = s;
-  }
-  if constexpr (LISTS) {
+  const size_t o = (size_t)row * p.ntiles + tile;
+  int n = 0;
+  if constexpr (TOP) {
+    const int K = p.K, cap = list_cap(K);
     auto id_of = [&](int i) { return tk.at(i / VEC) + i % VEC; };
-    uint32_t key = __builtin_bit_cast(uint32_t, m), th = 0;
-    key ^= key >> 31 ? 0xffffffffu : 0x80000000u;
-    for (int b = 31; b >= 0; --b) {
-      const uint32_t t = th | 1u << b;
-      if (__popcll(__ballot(key >= t)) >= K) th = t;
+    float theta = ninf;
+    if (K <= 8) {
+      float c = fmaxf(m, __shfl_xor(m, 16, kWave));
+      c = fmaxf(c, __shfl_xor(c, 32, kWave));      // every row of 16 lanes holds the 16 groups' maxima
+      for (int k = 0; k < 4 * K; k += taken(c, theta)) theta = row_max(c);
+    } else {
+      float c = m;
+      for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
     }
-    th ^= th >> 31 ? 0x80000000u : 0xffffffffu;
-    const float theta = __builtin_bit_cast(float, th);
+    theta = fmaxf(theta, -3.402823466e38f);        // -inf is no candidate
     const unsigned long long below = lane == 0 ? 0ull : (~0ull >> (64 - lane));
-    int n = 0;
+    uint2* list = p.list + o * cap;
 #pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
-      const bool keep = v[i] >= theta && v[i] > ninf;
+    for (int i = 0; i < PER; ++i) {
+      const bool keep = v[i] >= theta;
       const unsigned long long who = __ballot(keep);
       if (who) {
         const int pos = n + __popcll(who & below);
-        if (keep && pos < kWave) {
-          sv[w][pos] = v[i];
-          si[w][pos] = id_of(i);
-        }
+        if (keep && pos < cap) list[pos] = make_uint2(__builtin_bit_cast(uint32_t, v[i]), (uint32_t)id_of(i));
         n += __popcll(who);
       }
     }
-    __builtin_amdgcn_wave_barrier();
-    float lv = ninf;
-    int li = kNoId;
-    if (n <= kWave) {
-      const float a = lane < n ? sv[w][lane] : ninf;
-      const int id = lane < n ? si[w][lane] : kNoId;
-      int r = 0;
-      for (int d = 0; d < n; ++d) r += before(readlane_f(a, d), readlane_i(id, d), a, id) ? 1 : 0;
-      __builtin_amdgcn_wave_barrier();
-      if (lane < n && r < K) {
-        sv[w][r] = a;
-        si[w][r] = id;
-      }
-      __builtin_amdgcn_wave_barrier();
-      if (lane < min(n, K)) {
-        lv = sv[w][lane];
-        li = si[w][lane];
-      }
-    } else {
+    if (n > cap) {
       float pv = __builtin_inff();
       int pi = -1;
-      for (int k = 0; k < K; ++k) {
+      for (n = 0; n < K; ++n) {
         float bv = ninf;
         int bi = kNoId;
 #pragma unroll
-        for (int i = 0; i < kPerLane; ++i)
+        for (int i = 0; i < PER; ++i)
           if (v[i] > ninf && before(pv, pi, v[i], id_of(i)) && before(v[i], id_of(i), bv, bi)) {
             bv = v[i];
             bi = id_of(i);
@@ -248,50 +343,149 @@ __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const
             bi = oi;
           }
         }
-        if (lane == k) {
-          lv = bv;
-          li = bi;
-        }
+        if (lane == 0) list[n] = make_uint2(__builtin_bit_cast(uint32_t, bv), (uint32_t)bi);
         pv = bv;
         pi = bi;
       }
     }
-    if (lane < K) {
-      pval[o * K + lane] = lv;
-      pid[o * K + lane] = li;
-    }
+  }
+  if (lane == 0) {
+    p.max[o] = top;
+    p.sum[o] = s;
+    if (TOP) p.count[o] = n;
   }
 }
 
-// log-probabilities: the logits under the rules again, less the row's logsumexp, which every wave forms from the partials.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, const T* x, int64_t ld, int V, int slices, int ntiles,
-                                                              const float* __restrict__ pmax, const float* __restrict__ psum,
-                                                              float* logp, int64_t ld_out, float* __restrict__ lse_out) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-  const int row = blockIdx.x / slices;
-  const Tokens<T> tk(blockIdx.x % slices);
-  constexpr int VEC = Tokens<T>::VEC, NV = Tokens<T>::NV;
-  const float ninf = -__builtin_inff();
+// The row's logsumexp from its partials, in every lane.
+__device__ __forceinline__ float row_lse(const float* __restrict__ mx, const float* __restrict__ sm, int ntiles) {
   const int lane = threadIdx.x & 63;
-  float v[kPerLane];
-  ruled(q, x + (int64_t)row * ld, V, row, tk, lds, v);
+  const float ninf = -__builtin_inff();
   float m = ninf, s = 0.f;
-  for (int t = lane; t < ntiles; t += kWave) m = fmaxf(m, pmax[(size_t)row * ntiles + t]);
+  for (int t = lane; t < ntiles; t += kWave) m = fmaxf(m, mx[t]);
   m = wave_max(m);
   const float shift = m > ninf ? m : 0.f;
-  for (int t = lane; t < ntiles; t += kWave) s += psum[(size_t)row * ntiles + t] * __expf(pmax[(size_t)row * ntiles + t] - shift);
-  const float lse = shift + logf(wave_sum(s));
+  for (int t = lane; t < ntiles; t += kWave) s += sm[t] * __expf(mx[t] - shift);
+  return shift + logf(wave_sum(s));
+}
+
+// One wave per row: the lists of the tiles whose maximum reaches the K-th largest tile maximum hold the row's K largest values;
+// those that reach it too are ranked against each other. Where ties make that too many, K rounds of an argmax over all lists.
+constexpr int kMergeWaves = 4, kMergeTiles = 256, kMergeCands = 256;
+
+__global__ __launch_bounds__(kMergeWaves * kWave) void k_rules_merge(RulePartials p, int N, float* __restrict__ out,
+                                                                     int32_t* __restrict__ out_id, float* __restrict__ out_lse) {
+  __shared__ int qt[kMergeWaves][kMergeTiles];
+  __shared__ uint2 sv[kMergeWaves][kMergeCands];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int row = blockIdx.x * kMergeWaves + w;
+  if (row >= N) return;
+  const float ninf = -__builtin_inff();
+  const int K = p.K, cap = list_cap(K);
+  const float* mx = p.max + (size_t)row * p.ntiles;
+  const int* cnt = p.count + (size_t)row * p.ntiles;
+  const uint2* lists = p.list + (size_t)row * p.ntiles * cap;
+  const float lse = row_lse(mx, p.sum + (size_t)row * p.ntiles, p.ntiles);
+  float c = ninf, theta = ninf;
+  for (int t = lane; t < p.ntiles; t += kWave) c = fmaxf(c, mx[t]);
+  for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
+  const unsigned long long below = lane == 0 ? 0ull : (~0ull >> (64 - lane));
+  int nq = 0, n = 0;
+  for (int t0 = 0; t0 < p.ntiles; t0 += kWave) {
+    const int t = t0 + lane;
+    const bool q = t < p.ntiles && mx[t] >= theta && mx[t] > ninf;
+    const unsigned long long who = __ballot(q);
+    const int pos = nq + __popcll(who & below);
+    if (q && pos < kMergeTiles) qt[w][pos] = t;
+    nq += __popcll(who);
+  }
+  __builtin_amdgcn_wave_barrier();
+  if (nq <= kMergeTiles)
+    for (int s0 = 0; s0 < nq * cap && n <= kMergeCands; s0 += kWave) {
+      const int e = s0 + lane, t = e < nq * cap ? qt[w][e / cap] : 0;
+      uint2 a = make_uint2(0xff800000u, 0);
+      if (e < nq * cap && e % cap < cnt[t]) a = lists[(size_t)t * cap + e % cap];
+      const float v = __builtin_bit_cast(float, a.x);
+      const bool keep = v >= theta && v > ninf;
+      const unsigned long long who = __ballot(keep);
+      const int pos = n + __popcll(who & below);
+      if (keep && pos < kMergeCands) sv[w][pos] = a;
+      n += __popcll(who);
+    }
+  __builtin_amdgcn_wave_barrier();
+  float* o = out + (size_t)row * K;
+  int32_t* oi = out_id + (size_t)row * K;
+  if (nq <= kMergeTiles && n <= kMergeCands) {
+    for (int c0 = lane; c0 < n; c0 += kWave) {
+      const uint2 a = sv[w][c0];
+      const float v = __builtin_bit_cast(float, a.x);
+      int r = 0;
+      for (int d = 0; d < n; ++d) r += before(__builtin_bit_cast(float, sv[w][d].x), (int)sv[w][d].y, v, (int)a.y) ? 1 : 0;
+      if (r < K) {
+        o[r] = v - lse;
+        oi[r] = (int)a.y;
+      }
+    }
+    if (lane >= n && lane < K) {
+      o[lane] = ninf;
+      oi[lane] = kNoId;
+    }
+  } else {
+    float pv = __builtin_inff();
+    int pi = -1;
+    for (int k = 0; k < K; ++k) {
+      float bv = ninf;
+      int bi = kNoId;
+      for (int e = lane; e < p.ntiles * cap; e += kWave) {
+        if (e % cap >= cnt[e / cap]) continue;
+        const uint2 a = lists[e];
+        const float v = __builtin_bit_cast(float, a.x);
+        if (v > ninf && before(pv, pi, v, (int)a.y) && before(v, (int)a.y, bv, bi)) {
+          bv = v;
+          bi = (int)a.y;
+        }
+      }
+#pragma unroll
+      for (int d = kWave / 2; d > 0; d >>= 1) {
+        const float ov = __shfl_xor(bv, d, kWave);
+        const int od = __shfl_xor(bi, d, kWave);
+        if (before(ov, od, bv, bi)) {
+          bv = ov;
+          bi = od;
+        }
+      }
+      if (lane == 0) {
+        o[k] = bi == kNoId ? ninf : bv - lse;
+        oi[k] = bi;
+      }
+      pv = bv;
+      pi = bi;
+    }
+  }
+  if (out_lse && lane == 0) out_lse[row] = lse;
+}
+
+// log-probabilities: the logits under the rules again, less the row's logsumexp, which every wave forms from the partials.
+template <class T, int PER, bool LISTS>
+__global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, const T* x, int64_t ld, int V, int slices,
+                                                              RulePartials p, float* logp, int64_t ld_out,
+                                                              float* __restrict__ lse_out) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int row = blockIdx.x / slices;
+  constexpr int VEC = 4, NV = PER / VEC;       // 16-byte stores
+  const Tokens<PER, VEC> tk(blockIdx.x % slices);
+  const float ninf = -__builtin_inff();
+  float v[PER];
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
+  const float lse = row_lse(p.max + (size_t)row * p.ntiles, p.sum + (size_t)row * p.ntiles, p.ntiles);
   if (lse_out && tk.slice0 == 0 && threadIdx.x == 0) lse_out[row] = lse;
   float* o = logp + (int64_t)row * ld_out;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) v[i] = v[i] == ninf ? ninf : v[i] - lse;
+  for (int i = 0; i < PER; ++i) v[i] = v[i] == ninf ? ninf : v[i] - lse;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     const int t = tk.at(u);
     if (t + VEC <= V) {
-#pragma unroll
-      for (int i = 0; i < VEC; i += 4) store_vec(o + t + i, &v[u * VEC + i]);
+      store_vec(o + t, &v[u * VEC]);
     } else {
 #pragma unroll
       for (int i = 0; i < VEC; ++i)
@@ -300,45 +494,86 @@ __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, cons
   }
 }
 
-static unsigned lds_bytes(const LogitRules& r) { return ((r.history != nullptr) + (r.n_bias > 0)) * kSlice * 4; }
-static int slices_of(int V) { return (V + kSlice - 1) / kSlice; }
-static int tiles_of(int V) { return (V + kRuleTile - 1) / kRuleTile; }
+static bool has_lists(const LogitRules& r) { return r.history || r.n_bias > 0; }
 
+// Tokens per lane: 16, or 32 where candidates are chosen among logits without lists and every CU still gets workgroups enough:
+// that halves what a tile costs beside its logits (2560 x 50000 bf16, K = 5: 65 us against 81, K = 16: 104 against 144). With
+// lists the LDS of a slice of twice the size halves the workgroups per CU (every rule: 173 us against 137); without candidates
+// there is nothing to halve (logits alone 94 us against 89).
+static int per_lane(const LogitRules& r, int N, int V, int K) {
+  const int64_t slices = (V + 32 * kThreads - 1) / (32 * kThreads) * (int64_t)N;
+  return K > 0 && !has_lists(r) && slices >= 1024 ? 32 : 16;
+}
+
+// f(a null pointer of the logits' type, tokens per lane and whether there are lists as types, slices, LDS bytes)
 template <class F>
-static hipError_t by_type(int dtype, F&& f) {
-  if (dtype == kF32) f((float*)nullptr);
-  else if (dtype == kBF16) f((bf16_t*)nullptr);
-  else f((f16_t*)nullptr);
+static hipError_t by_type(const LogitRules& r, const LogitMat& m, int K, F&& f) {
+  auto run = [&](auto* t, auto per, auto lists) {
+    constexpr int P = decltype(per)::value;
+    f(t, per, lists, (m.V + P * kThreads - 1) / (P * kThreads), decltype(lists)::value ? (int)sizeof(RuleLds<P>) : 0);
+  };
+  auto g = [&](auto* t) {
+    if (has_lists(r)) run(t, Const<16>{}, Const<1>{});
+    else if (per_lane(r, m.N, m.V, K) == 16) run(t, Const<16>{}, Const<0>{});
+    else run(t, Const<32>{}, Const<0>{});
+  };
+  if (m.dtype == kF32) g((float*)nullptr);
+  else if (m.dtype == kBF16) g((bf16_t*)nullptr);
+  else g((f16_t*)nullptr);
   return hipGetLastError();
 }
 
+static size_t partials_layout(int N, int V, int K, int per, char* base, RulePartials* p) {
+  const int tile = per * kWave, nt = (V + tile - 1) / tile;
+  const size_t n = (size_t)N * nt, list = n * list_cap(K) * sizeof(uint2);      // the 8-byte entries first
+  if (p) *p = RulePartials{(uint2*)base, (float*)(base + list), (float*)(base + list) + n, (int*)(base + list) + 2 * n, nt, K};
+  return list + n * (K > 0 ? 12 : 8);
+}
+
+size_t rules_ws(int N, int V, int K) { return partials_layout(N, V, K, 16, nullptr, nullptr); }
+
+#define ONMT_TYPES(t, per, lists)                         \
+  using T = std::remove_pointer_t<decltype(t)>;           \
+  constexpr int P = decltype(per)::value;                 \
+  constexpr bool L = decltype(lists)::value != 0
+
 hipError_t rules_logits(const LogitRules& r, const LogitMat& m, void* out, int64_t ld_out, hipStream_t st) {
-  const int sl = slices_of(m.V);
-  return by_type(m.dtype, [&](auto* t) {
-    using T = std::remove_pointer_t<decltype(t)>;
-    hipLaunchKernelGGL(k_rules_logits<T>, dim3(m.N * sl), dim3(kThreads), lds_bytes(r), st, r, (const T*)m.x, m.ld, m.V, sl,
+  return by_type(r, m, 0, [&](auto* t, auto per, auto lists, int sl, int lds) {
+    ONMT_TYPES(t, per, lists);
+    hipLaunchKernelGGL((k_rules_logits<T, P, L>), dim3(m.N * sl), dim3(kThreads), lds, st, r, (const T*)m.x, m.ld, m.V, sl,
                        (T*)out, ld_out);
   });
 }
 
-hipError_t rules_partials(const LogitRules& r, const LogitMat& m, int K, float* pmax, float* psum, float* pval, int32_t* pid,
-                          hipStream_t st) {
-  const int sl = slices_of(m.V), nt = tiles_of(m.V);
-  return by_type(m.dtype, [&](auto* t) {
-    using T = std::remove_pointer_t<decltype(t)>;
-    const auto kernel = K > 0 ? k_rules_partials<T, true> : k_rules_partials<T, false>;
-    hipLaunchKernelGGL(kernel, dim3(m.N * sl), dim3(kThreads), lds_bytes(r), st, r, (const T*)m.x, m.ld, m.V, sl, nt, K, pmax,
-                       psum, pval, pid);
+// The first pass, and where it left its results in ws.
+static hipError_t partials(const LogitRules& r, const LogitMat& m, int K, void* ws, RulePartials* p, hipStream_t st) {
+  partials_layout(m.N, m.V, K, per_lane(r, m.N, m.V, K), (char*)ws, p);
+  return by_type(r, m, K, [&](auto* t, auto per, auto lists, int sl, int lds) {
+    ONMT_TYPES(t, per, lists);
+    const auto kernel = K > 0 ? k_rules_partials<T, P, L, true> : k_rules_partials<T, P, L, false>;
+    hipLaunchKernelGGL(kernel, dim3(m.N * sl), dim3(kThreads), lds, st, r, (const T*)m.x, m.ld, m.V, sl, *p);
   });
 }
 
-hipError_t rules_log_probs(const LogitRules& r, const LogitMat& m, const float* pmax, const float* psum, float* logp,
-                           int64_t ld_out, float* lse, hipStream_t st) {
-  const int sl = slices_of(m.V), nt = tiles_of(m.V);
-  return by_type(m.dtype, [&](auto* t) {
-    using T = std::remove_pointer_t<decltype(t)>;
-    hipLaunchKernelGGL(k_rules_log_probs<T>, dim3(m.N * sl), dim3(kThreads), lds_bytes(r), st, r, (const T*)m.x, m.ld, m.V, sl,
-                       nt, pmax, psum, logp, ld_out, lse);
+hipError_t rules_top(const LogitRules& r, const LogitMat& m, int K, void* ws, float* out, int32_t* ids, float* lse,
+                     hipStream_t st) {
+  RulePartials p;
+  const hipError_t e = partials(r, m, K, ws, &p, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_rules_merge, dim3((m.N + kMergeWaves - 1) / kMergeWaves), dim3(kMergeWaves * kWave), 0, st, p, m.N, out,
+                     ids, lse);
+  return hipGetLastError();
+}
+
+hipError_t rules_log_probs(const LogitRules& r, const LogitMat& m, void* ws, float* logp, int64_t ld_out, float* lse,
+                           hipStream_t st) {
+  RulePartials p;
+  const hipError_t e = partials(r, m, 0, ws, &p, st);
+  if (e != hipSuccess) return e;
+  return by_type(r, m, 0, [&](auto* t, auto per, auto lists, int sl, int lds) {
+    ONMT_TYPES(t, per, lists);
+    hipLaunchKernelGGL((k_rules_log_probs<T, P, L>), dim3(m.N * sl), dim3(kThreads), lds, st, r, (const T*)m.x, m.ld, m.V, sl, p,
+                       logp, ld_out, lse);
   });
 }
 
