@@ -285,8 +285,8 @@ enum { ONMT_F32 = 0, ONMT_BF16 = 1, ONMT_F16 = 2 };
  *   out[m, n] = sum_k x8[m, k] w8[n, k] + bias[n]      (m < M, n < rows, k < cols; bias fp32 or NULL)
  * with x8 = x in the same form, accumulated in fp32 and rounded once to out's type (bf16 and fp16 results: blocks of 128
  * products are summed by the 8-bit matrix instruction, off by some 1.5e-5 of a sum's rms). ws holds onmt_f8_linear_ws_bytes(M, cols) bytes
- * of scratch, 16-byte aligned; out overlaps neither x nor ws nor packed. All are asynchronous on the stream and may be captured;
- * calls that share no ws and no output may run at the same time. Sizes: up to 2^24 blocks of 16 rows x 128 columns per operand
+ * of scratch, 16-byte aligned (where that is 0, ws may be NULL); out overlaps neither x nor ws nor packed. All are asynchronous on the stream and may be captured;
+ * calls that share no ws and no output may run at the same time. Sizes: up to 2^20 columns, 2^24 blocks of 16 rows x 128 columns per operand
  * and 2^24 tiles of 16 x 64 outputs (ONMT_EUNSUPPORTED beyond). */
 size_t onmt_f8_bytes(int rows, int cols);
 int onmt_f8_pack(const void* w, int dtype, int64_t ld, int rows, int cols, void* packed, size_t packed_bytes, void* stream);

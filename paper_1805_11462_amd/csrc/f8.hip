@@ -17,7 +17,10 @@
 // the powers (biased by 127), one byte per row and block: the four blocks 4 j .. 4 j + 3 of a row are a dword, which the
 // instruction picks its byte from, the dwords of 16 rows side by side.
 
+#include <type_traits>
+
 #include "common.h"
+#include "gemm_device.h"
 #include "kernels.h"
 #include "types.h"
 
@@ -53,36 +56,23 @@ __device__ __forceinline__ void f8_round(const float (&x)[32], int e, i32x4& lo,
   hi = q[1];
 }
 
-// Four e4m3 values times 2^(biased - 127) as bf16.
-__device__ __forceinline__ int2 f8_widen(int w, int biased) {
-  const float s = __builtin_bit_cast(float, biased << 23);
-  return make_int2(__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false)),
-                   __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)));
-}
-
-// One wave per fragment block. WIDE: the values as bf16 with their powers, in blocks of twice the size: 16 bytes per lane and
-// quarter of the lane's 32 columns, a kilobyte per quarter; no powers.
-template <class T, bool WIDE>
-__global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_t ld, int rows, int cols, F8Mat out, int nblocks) {
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (b >= nblocks) return;
-  const int rb = b / out.kblocks, kb = b % out.kblocks;
-  const int r = rb * 16 + (lane & 15), g = lane >> 4;
-  const int k0 = kb * kF8Block + 32 * g;
-  float v[32];
+// Entries k0 .. k0 + 31 of a row of `cols` columns, zeros past them, clamped to finite values.
+template <class T>
+__device__ __forceinline__ void load32(const T* row, int k0, int cols, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = 0.f;
-  if (r < rows) {
-    const T* p = x + (int64_t)r * ld + k0;
-    if (k0 + 32 <= cols) {
+  if (k0 + 32 <= cols) {
 #pragma unroll
-      for (int i = 0; i < 32; i += kVec<T>) load_vec(p + i, &v[i]);
-    } else {
+    for (int i = 0; i < 32; i += kVec<T>) load_vec(row + k0 + i, &v[i]);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (k0 + i < cols) v[i] = to_float(p[i]);
-    }
+    for (int i = 0; i < 32; ++i)
+      if (k0 + i < cols) v[i] = to_float(row[k0 + i]);
   }
+}
+
+// A wave's fragment block from its entries: lo, hi, and the power of the lane's row.
+__device__ __forceinline__ int f8_block(float (&v)[32], i32x4& lo, i32x4& hi) {
   float a = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
@@ -92,24 +82,26 @@ __global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_
   a = fmaxf(a, __shfl_xor(a, 16, kWave));
   a = fmaxf(a, __shfl_xor(a, 32, kWave));
   const int e = f8_exp(a);
-  i32x4 lo, hi;
   f8_round(v, e, lo, hi);
-  if constexpr (WIDE) {
-    char* d = out.data + (size_t)b * (2 * kF8Frag) + lane * 16;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const i32x4& h = i < 2 ? lo : hi;
-      const int2 p = f8_widen(h[2 * (i & 1)], kF8One + e), q = f8_widen(h[2 * (i & 1) + 1], kF8One + e);
-      *(i32x4*)(d + i * 1024) = i32x4{p.x, p.y, q.x, q.y};
-    }
-    return;
-  }
+  return e;
+}
+
+// One wave per fragment block.
+template <class T>
+__global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_t ld, int rows, int cols, F8Mat out, int nblocks) {
+  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (b >= nblocks) return;
+  const int rb = b / out.kblocks, kb = b % out.kblocks;
+  const int r = rb * 16 + (lane & 15), g = lane >> 4;
+  float v[32];
+  load32(x + (int64_t)min(r, rows - 1) * ld, kb * kF8Block + 32 * g, r < rows ? cols : 0, v);
+  i32x4 lo, hi;
+  const int e = f8_block(v, lo, hi);
   char* d = out.data + (size_t)b * kF8Frag + lane * 16;
   *(i32x4*)d = lo;
   *(i32x4*)(d + kF8Frag / 2) = hi;
   if (g == 0) {
-    const int kq = out.kquads();
-    uint8_t* s = (uint8_t*)(out.exps + ((size_t)rb * kq + kb / 4) * 16 + lane);
+    uint8_t* s = (uint8_t*)(out.exps + ((size_t)rb * out.kquads() + kb / 4) * 16 + lane);
     s[kb & 3] = (uint8_t)(kF8One + e);
     if (kb == out.kblocks - 1)
       for (int j = (kb & 3) + 1; j < 4; ++j) s[j] = kF8One;
@@ -131,9 +123,27 @@ __global__ __launch_bounds__(256) void k_f8_unpack(F8Mat w, int rows, int cols, 
   for (int j = 0; j < 4 && c + j < cols; ++j) out[(int64_t)r * ld + c + j] = ldexpf(v[j], e);
 }
 
-template <int J>
-__device__ __forceinline__ f32x4 mfma_f8(const i32x8& w, const i32x8& x, const f32x4& c, int we, int xe) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, J, we, J, xe);
+// ------------------------------------------------------------------------------------------------- products
+// The weights are the instruction's row operand: lane (i16, g) ends up with columns 4 g .. + 3 of row i16 of a 16 x 16 tile.
+
+// A lane's 32 values as bf16, times 2^(biased - 127): the operands of four 32-column products.
+struct Wide8 {
+  bf16x8 q[4];
+};
+__device__ __forceinline__ Wide8 f8_widen(const i32x8& f, int biased) {
+  const float s = __builtin_bit_cast(float, biased << 23);
+  Wide8 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    i32x4 p;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      p[2 * h] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + h], s, false));
+      p[2 * h + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + h], s, true));
+    }
+    w.q[i] = __builtin_bit_cast(bf16x8, p);
+  }
+  return w;
 }
 
 __device__ __forceinline__ i32x8 f8_frag(const char* p) {
@@ -141,58 +151,226 @@ __device__ __forceinline__ i32x8 f8_frag(const char* p) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// One wave per 16 rows x 16 TN columns. The weights are the instruction's row operand: lane (i16, g) ends up with columns
-// 4 g .. + 3 of row i16.
-constexpr int kTN = 4;
-
-template <class T>
-__global__ __launch_bounds__(256) void k_f8_linear(F8Mat x, F8Mat w, int M, int N, const float* __restrict__ bias,
-                                                   T* __restrict__ out, int64_t ld, int nm, int ntiles) {
-  constexpr bool WIDE = sizeof(T) == 4;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t >= ntiles) return;
-  const int mb = t % nm, nb0 = t / nm * kTN, nrb = (N + 15) / 16;
-  const int kb = x.kblocks, kq = x.kquads();
-  const int i16 = lane & 15, g = lane >> 4;
-  const char* xp = x.data + (size_t)mb * kb * (WIDE ? 2 * kF8Frag : kF8Frag) + lane * 16;
-  const int* xe = x.exps + (size_t)mb * kq * 16 + i16;
-  const char* wp[kTN];
-  const int* we[kTN];
-  f32x4 c[kTN];
+// c[x][y] += products of one 128-column block: rows' fragments a[x] and weights' w[y], byte J of their powers.
+template <bool EXACT, int J, int TM, int TN>
+__device__ __forceinline__ void f8_multiply(f32x4 (&c)[TM][TN], const i32x8 (&a)[TM], const int (&ea)[TM], const i32x8 (&w)[TN],
+                                            const int (&ew)[TN]) {
+  if constexpr (EXACT) {
+    Wide8 ww[TN];
 #pragma unroll
-  for (int y = 0; y < kTN; ++y) {
-    const size_t rb = min(nb0 + y, nrb - 1);
-    wp[y] = w.data + rb * kb * kF8Frag + lane * 16;
-    we[y] = w.exps + rb * kq * 16 + i16;
-    c[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int y = 0; y < TN; ++y) ww[y] = f8_widen(w[y], ew[y] >> (8 * J) & 255);
+#pragma unroll
+    for (int x = 0; x < TM; ++x) {
+      const Wide8 aw = f8_widen(a[x], ea[x] >> (8 * J) & 255);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int y = 0; y < TN; ++y) c[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww[y].q[i], aw.q[i], c[x][y], 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+      for (int y = 0; y < TN; ++y)
+        c[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[y], a[x], c[x][y], 0, 0, J, ew[y], J, ea[x]);
   }
-  for (int q = 0; q < kq; ++q) {
-    const int ex = WIDE ? 0 : xe[q * 16];
-    int ew[kTN];
+}
+
+template <class T, int N>
+struct Packed {
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// Four biases from column n on, zeros past N.
+__device__ __forceinline__ f32x4 bias4(const float* __restrict__ bias, int N, int n) {
+  f32x4 b{0.f, 0.f, 0.f, 0.f};
+  if (bias) {
+    if (n + 4 <= N) {
+      b = *(const Packed<float, 4>::type*)(bias + n);
+    } else {
 #pragma unroll
-    for (int y = 0; y < kTN; ++y) ew[y] = we[y][q * 16];
+      for (int j = 0; j < 4; ++j)
+        if (n + j < N) b[j] = bias[n + j];
+    }
+  }
+  return b;
+}
+
+// Few rows (up to 16 TM): the weights' stream is the bound (25.6 MB at 50000 x 500), so each wave loads those of its own 16
+// columns straight into registers, four blocks at a time and the next four before it multiplies. The workgroup rounds all rows
+// to 8 bits itself, into LDS, while its first weights are on their way: a launch less, and every workgroup reads the rows from
+// the caches.
+template <class X, class T, int TM>
+__global__ __launch_bounds__(256) void k_f8_few(const X* __restrict__ x, int64_t ldx, F8Mat w, int M, int N, int cols,
+                                                const float* __restrict__ bias, T* __restrict__ out, int64_t ld) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  constexpr bool EXACT = sizeof(T) == 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g = lane >> 4;
+  const int kb = w.kblocks, kq = w.kquads(), nrb = (N + 15) / 16;
+  const int nb = min(blockIdx.x * 4 + wave, nrb - 1);
+  const char* wp = w.data + (size_t)nb * kb * kF8Frag + lane * 16;
+  const int* we = w.exps + (size_t)nb * kq * 16 + i16;
+  i32x8 f[2][4];
+  int ew[2];
+  auto load = [&](int q, i32x8 (&r)[4], int& e) {
+    e = we[min(q, kq - 1) * 16];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = f8_frag(wp + (size_t)min(4 * q + j, kb - 1) * kF8Frag);
+  };
+  load(0, f[0], ew[0]);
+  const f32x4 b4 = bias4(bias, N, nb * 16 + 4 * g);
+  // rows: fragment blocks [kb][TM], then the powers [TM][kq][16] as in a packed matrix
+  int* le = (int*)(lds + (size_t)kb * TM * kF8Frag);
+  for (int b = wave; b < kb * TM; b += 4) {
+    const int rb = b % TM, k = b / TM, r = rb * 16 + i16;
+    float v[32];
+    load32(x + (int64_t)min(r, M - 1) * ldx, k * kF8Block + 32 * g, r < M ? cols : 0, v);
+    i32x4 lo, hi;
+    const int e = f8_block(v, lo, hi);
+    *(i32x4*)(lds + (size_t)b * kF8Frag + lane * 16) = lo;
+    *(i32x4*)(lds + (size_t)b * kF8Frag + kF8Frag / 2 + lane * 16) = hi;
+    if (g == 0) ((uint8_t*)(le + (rb * kq + k / 4) * 16 + i16))[k & 3] = (uint8_t)(kF8One + e);
+  }
+  __syncthreads();
+  f32x4 c[TM][1];
+#pragma unroll
+  for (int t = 0; t < TM; ++t) c[t][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto quad = [&](int q, const i32x8 (&r)[4], int e) {
+    int ea[TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) ea[t] = le[(t * kq + q) * 16 + i16];
     auto step = [&](auto j) {
       constexpr int J = decltype(j)::value;
       const int k = 4 * q + J;
       if (k >= kb) return;
-      if constexpr (WIDE) {
-        bf16x8 a[4];
+      i32x8 a[TM];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = *(const bf16x8*)(xp + (size_t)k * (2 * kF8Frag) + i * 1024);
+      for (int t = 0; t < TM; ++t) a[t] = f8_frag(lds + (size_t)(k * TM + t) * kF8Frag + lane * 16);
+      const i32x8 b[1] = {r[J]};
+      const int eb[1] = {e};
+      f8_multiply<EXACT, J, TM, 1>(c, a, ea, b, eb);
+    };
+    step(Const<0>{});
+    step(Const<1>{});
+    step(Const<2>{});
+    step(Const<3>{});
+  };
+  for (int q = 0; q < kq; q += 2) {
+    if (q + 1 < kq) load(q + 1, f[1], ew[1]);
+    quad(q, f[0], ew[0]);
+    if (q + 1 < kq) {
+      if (q + 2 < kq) load(q + 2, f[0], ew[0]);
+      quad(q + 1, f[1], ew[1]);
+    }
+  }
+  if (blockIdx.x * 4 + wave >= nrb) return;
+  const int n = nb * 16 + 4 * g;
 #pragma unroll
-        for (int y = 0; y < kTN; ++y) {
-          const i32x8 b = f8_frag(wp[y] + (size_t)k * kF8Frag);
+  for (int t = 0; t < TM; ++t) {
+    const int m = t * 16 + i16;
+    if (m >= M) break;
+    const f32x4 v = c[t][0] + b4;
+    T* p = out + (int64_t)m * ld + n;
+    if (n + 4 <= N) {
+      typename Packed<T, 4>::type o;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int2 p = f8_widen(b[2 * i], ew[y] >> (8 * J) & 255), r = f8_widen(b[2 * i + 1], ew[y] >> (8 * J) & 255);
-            c[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, i32x4{p.x, p.y, r.x, r.y}), a[i], c[y], 0,
-                                                           0, 0);
-          }
+      for (int j = 0; j < 4; ++j) o[j] = from_float<T>(v[j]);
+      *(typename Packed<T, 4>::type*)p = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < N) p[j] = from_float<T>(v[j]);
+    }
+  }
+}
+
+// Many rows: 16 WM TM x 16 WN TN tiles of WM x WN waves, both operands through LDS in two stages of one 128-column block, moved
+// there by LDS-destination loads: a stage's loads are issued right behind the barrier that frees its buffer and are in flight
+// while the other stage is multiplied.
+template <int TM_, int TN_, int WM_, int WN_>
+struct F8Tile {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NT = 64 * WM * WN;
+  static constexpr int RB = WM * TM, CB = WN * TN, BM = 16 * RB, BN = 16 * CB;
+  static constexpr int STG = (RB + CB) * kF8Frag, LDS = 2 * STG;
+  static constexpr int LPW = 2 * (RB + CB) / (WM * WN);          // 1 KB loads per wave and stage
+  static_assert(LPW * WM * WN == 2 * (RB + CB), "whole loads");
+};
+
+template <class C, class T>
+__global__ __launch_bounds__(C::NT) void k_f8_wide(F8Mat x, F8Mat w, int M, int N, const float* __restrict__ bias,
+                                                   T* __restrict__ out, int64_t ld, int nm, int nn, int band) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  constexpr int TM = C::TM, TN = C::TN, W = C::WM * C::WN;
+  __shared__ __attribute__((aligned(16))) char lds[C::LDS];
+  // tiles in bands of `band` row tiles, column tiles outer: what a band's rows and a few column tiles hold fits an XCD's L2
+  int t = xcd_remap(blockIdx.x, nm * nn);
+  const int b0 = t / (band * nn) * band, bh = min(band, nm - b0);
+  t -= b0 * nn;
+  const int rb0 = (b0 + t % bh) * C::RB, cb0 = t / bh * C::CB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g = lane >> 4, wm = wave % C::WM, wn = wave / C::WM;
+  const int kb = x.kblocks, kq = x.kquads(), nrb = (M + 15) / 16, ncb = (N + 15) / 16;
+
+  // load i of this wave moves half (w + W i) & 1 of block (w + W i) / 2 of the stage; row blocks past the operand's last
+  // re-read that (they are never stored)
+  const int nra = min(C::RB, nrb - rb0), nca = min(C::CB, ncb - cb0);
+  const uint32_t rowb = (uint32_t)kb * kF8Frag;
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(x.data + (size_t)rb0 * rowb, (uint32_t)nra * rowb);
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(w.data + (size_t)cb0 * rowb, (uint32_t)nca * rowb);
+  auto issue = [&](int st) {
+    char* base = lds + (st & 1) * C::STG;
+#pragma unroll
+    for (int i = 0; i < C::LPW; ++i) {
+      const int q = wave + W * i, b = q >> 1;
+      const uint32_t half = (q & 1) * (kF8Frag / 2);
+      if (b < C::RB) dma16(rx, base + q * (kF8Frag / 2), (uint32_t)min(b, nra - 1) * rowb + half + lane * 16u, (uint32_t)st * kF8Frag);
+      else dma16(rw, base + q * (kF8Frag / 2), (uint32_t)min(b - C::RB, nca - 1) * rowb + half + lane * 16u, (uint32_t)st * kF8Frag);
+    }
+  };
+  const int* xe[TM];
+  const int* we[TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a) xe[a] = x.exps + (size_t)min(rb0 + wm * TM + a, nrb - 1) * kq * 16 + i16;
+#pragma unroll
+  for (int a = 0; a < TN; ++a) we[a] = w.exps + (size_t)min(cb0 + wn * TN + a, ncb - 1) * kq * 16 + i16;
+
+  f32x4 c[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b) c[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  issue(0);
+  for (int q = 0; q < kq; ++q) {
+    int ea[TM], ew[TN];
+#pragma unroll
+    for (int a = 0; a < TM; ++a) ea[a] = xe[a][q * 16];
+#pragma unroll
+    for (int a = 0; a < TN; ++a) ew[a] = we[a][q * 16];
+    auto step = [&](auto j) {
+      constexpr int J = decltype(j)::value;
+      const int st = 4 * q + J;
+      if (st >= kb) return;
+      // this wave's loads of stage st have landed; behind the barrier everyone's have, and nobody reads the other buffer
+      __builtin_amdgcn_s_waitcnt(waitcnt_stage(0));
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (st + 1 < kb) issue(st + 1);
+      const char* base = lds + (st & 1) * C::STG + lane * 16;
+      i32x8 wf[TN], af[TM];
+#pragma unroll
+      for (int b = 0; b < TN; ++b) wf[b] = f8_frag(base + (C::RB + wn * TN + b) * kF8Frag);
+#pragma unroll
+      for (int a = 0; a < TM; ++a) af[a] = f8_frag(base + (wm * TM + a) * kF8Frag);
+      f8_multiply<EXACT, J, TM, TN>(c, af, ea, wf, ew);
+      if constexpr (!EXACT) {       // rows' fragments one ahead of the products that take them
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 4, 0);
+#pragma unroll
+        for (int a = 0; a < TM; ++a) {
+          __builtin_amdgcn_sched_group_barrier(0x008, TN, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
-      } else {
-        const i32x8 a = f8_frag(xp + (size_t)k * kF8Frag);
-#pragma unroll
-        for (int y = 0; y < kTN; ++y) c[y] = mfma_f8<J>(f8_frag(wp[y] + (size_t)k * kF8Frag), a, c[y], ew[y], ex);
       }
     };
     step(Const<0>{});
@@ -200,33 +378,67 @@ __global__ __launch_bounds__(256) void k_f8_linear(F8Mat x, F8Mat w, int M, int 
     step(Const<2>{});
     step(Const<3>{});
   }
-  const int m = mb * 16 + i16;
-  if (m >= M) return;
+  // the wave's 16 TM x 64 results through LDS, 16 bytes of a row per lane: whole 128-byte lines leave, where the accumulators'
+  // own layout has 8 or 16 bytes of 16 rows per store. Chunks of a row are swizzled by the row against bank conflicts.
+  constexpr int VEC = kVec<T>, CH = 16 * TN / VEC, RPI = kWave / CH;      // chunks per row, rows per store
+  static_assert(TN == 4 && W * 16 * TM * CH * 16 <= C::LDS, "a wave's results fit its part of LDS");
+  const int m0 = (rb0 + wm * TM) * 16, n0 = (cb0 + wn * TN) * 16;
+  f32x4 add[TN];
 #pragma unroll
-  for (int y = 0; y < kTN; ++y) {
-    const int n = (nb0 + y) * 16 + 4 * g;
+  for (int b = 0; b < TN; ++b) add[b] = bias4(bias, N, n0 + 16 * b + 4 * g);
+  __builtin_amdgcn_s_waitcnt(waitcnt_stage(63));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  char* mine = lds + wave * (16 * TM * CH * 16);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n + j < N) out[(int64_t)m * ld + n + j] = from_float<T>(c[y][j] + (bias ? bias[n + j] : 0.f));
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+      const f32x4 v = c[a][b] + add[b];
+      T o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = from_float<T>(v[j]);
+      const int r = 16 * a + i16, k = 16 * b + 4 * g;
+      __builtin_memcpy(__builtin_assume_aligned(mine + (r * CH + ((k / VEC) ^ (r & (CH - 1)))) * 16 + k % VEC * (int)sizeof(T), 4 * sizeof(T)), o, 4 * sizeof(T));
+    }
+  __builtin_amdgcn_wave_barrier();
+  const int rl = lane / CH, n = n0 + lane % CH * VEC;
+#pragma unroll 4
+  for (int it = 0; it < 16 * TM / RPI; ++it) {
+    const int r = it * RPI + rl, m = m0 + r;
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    const vec v = *(const vec*)(mine + (r * CH + ((lane % CH) ^ (r & (CH - 1)))) * 16);
+    if (m < M) {
+      T* p = out + (int64_t)m * ld + n;
+      if (n + VEC <= N) {
+        *(typename Packed<T, VEC>::type*)p = v;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (n + j < N) p[j] = v[j];
+      }
+    }
   }
 }
 
-template <class T>
-static hipError_t pack(const void* x, int64_t ld, int rows, int cols, bool wide, const F8Mat& out, hipStream_t st) {
-  const int nb = (rows + 15) / 16 * out.kblocks;
-  const auto kernel = wide ? k_f8_pack<T, true> : k_f8_pack<T, false>;
-  hipLaunchKernelGGL(kernel, dim3((nb + 3) / 4), dim3(256), 0, st, (const T*)x, ld, rows, cols, out, nb);
+// ------------------------------------------------------------------------------------------------- launches
+// f(a null pointer of the type)
+template <class F>
+static hipError_t f8_type(int dtype, F&& f) {
+  if (dtype == kF32) f((float*)nullptr);
+  else if (dtype == kBF16) f((bf16_t*)nullptr);
+  else f((f16_t*)nullptr);
   return hipGetLastError();
 }
-
-static hipError_t pack_any(const void* x, int dtype, int64_t ld, int rows, int cols, bool wide, const F8Mat& out, hipStream_t st) {
-  return dtype == kF32 ? pack<float>(x, ld, rows, cols, wide, out, st)
-         : dtype == kBF16 ? pack<bf16_t>(x, ld, rows, cols, wide, out, st)
-                          : pack<f16_t>(x, ld, rows, cols, wide, out, st);
-}
+#define ONMT_TYPE(p) std::remove_pointer_t<decltype(p)>
 
 hipError_t f8_pack(const void* x, int dtype, int64_t ld, int rows, int cols, const F8Mat& out, hipStream_t st) {
-  return pack_any(x, dtype, ld, rows, cols, false, out, st);
+  const int nb = (rows + 15) / 16 * out.kblocks;
+  return f8_type(dtype, [&](auto* t) {
+    using X = ONMT_TYPE(t);
+    hipLaunchKernelGGL(k_f8_pack<X>, dim3((nb + 3) / 4), dim3(256), 0, st, (const X*)x, ld, rows, cols, out, nb);
+  });
 }
 
 hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld, hipStream_t st) {
@@ -235,23 +447,48 @@ hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld,
   return hipGetLastError();
 }
 
-template <class T>
-static hipError_t linear(const F8Mat& x, const F8Mat& w, int M, int N, const float* bias, void* out, int64_t ld, hipStream_t st) {
-  const int nm = (M + 15) / 16, nt = nm * ((N + 16 * kTN - 1) / (16 * kTN));
-  hipLaunchKernelGGL(k_f8_linear<T>, dim3((nt + 3) / 4), dim3(256), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nt);
-  return hipGetLastError();
+// Rows whose 8-bit values a workgroup of k_f8_few holds in LDS beside their powers: 16, 32 or 64 of them, 0 if they are too many.
+constexpr int kFewLds = 64 << 10;
+static int few_rows(int M, int cols) {
+  const int tm = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  return M <= 64 && f8_data_bytes(16 * tm, cols) + f8_exp_bytes(16 * tm, cols) <= kFewLds ? tm : 0;
 }
 
-size_t f8_linear_ws(int M, int cols) { return 2 * f8_data_bytes(M, cols); }
+template <class X, class T, int TM>
+static void launch_few(const void* x, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out, int64_t ld,
+                       hipStream_t st) {
+  const int bytes = (int)(f8_data_bytes(16 * TM, cols) + f8_exp_bytes(16 * TM, cols));
+  hipLaunchKernelGGL((k_f8_few<X, T, TM>), dim3((N + 63) / 64), dim3(256), bytes, st, (const X*)x, ldx, w, M, N, cols, bias,
+                     (T*)out, ld);
+}
+
+template <class C, class T>
+static void launch_wide(const F8Mat& x, int M, const F8Mat& w, int N, const float* bias, void* out, int64_t ld, hipStream_t st) {
+  const int nm = (M + C::BM - 1) / C::BM, nn = (N + C::BN - 1) / C::BN;
+  hipLaunchKernelGGL((k_f8_wide<C, T>), dim3(nm * nn), dim3(C::NT), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nn, 8);
+}
+
+size_t f8_linear_ws(int M, int cols) { return few_rows(M, cols) ? 0 : f8_data_bytes(M, cols) + f8_exp_bytes(M, cols); }
 
 hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out,
                      int out_dtype, int64_t ld, void* ws, hipStream_t st) {
+  if (const int tm = few_rows(M, cols))
+    return f8_type(dtype, [&](auto* tx) {
+      f8_type(out_dtype, [&](auto* to) {
+        using X = ONMT_TYPE(tx);
+        using T = ONMT_TYPE(to);
+        (tm == 1 ? launch_few<X, T, 1> : tm == 2 ? launch_few<X, T, 2> : launch_few<X, T, 4>)(x, ldx, M, w, N, cols, bias, out, ld, st);
+      });
+    });
   const F8Mat xm = f8_mat(ws, M, cols);
-  const hipError_t e = pack_any(x, dtype, ldx, M, cols, out_dtype == kF32, xm, st);
+  const hipError_t e = f8_pack(x, dtype, ldx, M, cols, xm, st);
   if (e != hipSuccess) return e;
-  return out_dtype == kF32 ? linear<float>(xm, w, M, N, bias, out, ld, st)
-         : out_dtype == kBF16 ? linear<bf16_t>(xm, w, M, N, bias, out, ld, st)
-                              : linear<f16_t>(xm, w, M, N, bias, out, ld, st);
+  return f8_type(out_dtype, [&](auto* to) {
+    using T = ONMT_TYPE(to);
+    if constexpr (sizeof(T) == 2)
+      if (M > 256) return launch_wide<F8Tile<8, 4, 2, 4>, T>(xm, M, w, N, bias, out, ld, st);
+    launch_wide<F8Tile<4, 4, 2, 2>, T>(xm, M, w, N, bias, out, ld, st);
+  });
 }
 
 }  // namespace onmt

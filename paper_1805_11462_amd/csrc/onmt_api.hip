@@ -1252,9 +1252,11 @@ int check_beam(const onmt_model* m, int S, int K) {
 
 // ------------------------------------------------------------------ matrices of a caller's type, rules on logits
 constexpr int64_t kF8MaxBlocks = 1 << 24;
+constexpr int kF8MaxCols = 1 << 20;            // the products' offsets within a tile's rows are 32-bit byte counts
 constexpr int kMaxRuleVocab = 1 << 20, kMaxRuleList = 65535;      // lists: counts and entries share a word
 
 int64_t f8_blocks(int64_t rows, int64_t cols) { return ((rows + 15) / 16) * ((cols + kF8Block - 1) / kF8Block); }
+bool f8_fits(int64_t rows, int64_t cols) { return f8_blocks(rows, cols) <= kF8MaxBlocks && cols <= kF8MaxCols; }
 size_t elem_bytes(int dtype) { return dtype == ONMT_F32 ? 4 : 2; }
 
 // Device bytes [lo, hi).
@@ -1279,7 +1281,7 @@ int check_matrix(const char* name, const void* p, int dtype, int64_t ld, int row
 int check_packed(const void* packed, size_t bytes, int rows, int cols) {
   if (!packed || (uintptr_t)packed % 16) return fail(ONMT_EINVAL, "packed must be a 16-byte aligned device buffer");
   if (rows < 1 || cols < 1) return fail(ONMT_EINVAL, "a packed matrix needs at least one row and column");
-  if (f8_blocks(rows, cols) > kF8MaxBlocks) return fail(ONMT_EUNSUPPORTED, "a matrix of %d x %d is too large", rows, cols);
+  if (!f8_fits(rows, cols)) return fail(ONMT_EUNSUPPORTED, "a matrix of %d x %d is too large", rows, cols);
   const size_t need = f8_data_bytes(rows, cols) + f8_exp_bytes(rows, cols);
   if (bytes < need) return fail(ONMT_ESIZE, "packed holds %zu bytes, %zu are needed", bytes, need);
   return ONMT_OK;
@@ -1688,7 +1690,7 @@ int onmt_score(onmt_model* m, const int32_t* src, const int32_t* len, int B, int
 }
 
 size_t onmt_f8_bytes(int rows, int cols) {
-  if (f8_blocks(rows, cols) > kF8MaxBlocks || rows < 1 || cols < 1) return 0;
+  if (rows < 1 || cols < 1 || !f8_fits(rows, cols)) return 0;
   return f8_data_bytes(rows, cols) + f8_exp_bytes(rows, cols);
 }
 
@@ -1707,7 +1709,7 @@ int onmt_f8_unpack(const void* packed, size_t packed_bytes, int rows, int cols, 
 }
 
 size_t onmt_f8_linear_ws_bytes(int M, int cols) {
-  if (f8_blocks(M, cols) > kF8MaxBlocks || M < 1 || cols < 1) return 0;
+  if (M < 1 || cols < 1 || !f8_fits(M, cols)) return 0;
   return f8_linear_ws(M, cols);
 }
 
@@ -1717,10 +1719,10 @@ int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* pac
   if (rc || (rc = check_matrix("out", out, out_dtype, ld_out, M, rows)) || (rc = check_packed(packed, packed_bytes, rows, cols)))
     return rc;
   if ((uintptr_t)bias % sizeof(float)) return fail(ONMT_EINVAL, "bias is not aligned to its elements");
-  if (f8_blocks(M, cols) > kF8MaxBlocks || ((M + 15) / 16) * (int64_t)((rows + 63) / 64) > kF8MaxBlocks)
+  if (!f8_fits(M, cols) || ((M + 15) / 16) * (int64_t)((rows + 63) / 64) > kF8MaxBlocks)
     return fail(ONMT_EUNSUPPORTED, "a product of %d x %d by %d rows is too large", M, cols, rows);
-  if (!ws || (uintptr_t)ws % 16) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
   const size_t need = onmt_f8_linear_ws_bytes(M, cols);
+  if (need && (!ws || (uintptr_t)ws % 16)) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
   if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
   const Span so = span(out, out_dtype, ld_out, M, rows);
   if (so.meets(span(x, dtype, ldx, M, cols)) || so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need}) ||

@@ -6,6 +6,7 @@ columns and any row stride.
 """
 
 import ctypes
+import functools
 
 import torch
 
@@ -43,65 +44,61 @@ def _vector(name, t, n, dtype, device):
         raise ValueError(f"{name} must be a contiguous {dtype} vector" + (f" of {n}" if n is not None else ""))
 
 
-class _device:
-    """The tensors' GPU as the current one, where it is not."""
+# A decoding program makes these calls every step: sizes that depend on nothing else are asked once, and the stream's handle is
+# read without making a torch.cuda.Stream (9 of the 17 us that a small call took on the host).
+@functools.lru_cache(maxsize=4096)
+def _bytes_of(query, *sizes):
+    return getattr(_lib.load(), query)(*sizes)
 
-    def __init__(self, device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(device, function, *args):
+    """The library call with the tensors' GPU as the current one, on that GPU's current stream."""
+    if device.index == torch.cuda.current_device():
+        check(function(*args, torch._C._cuda_getCurrentRawStream(device.index)))
+    else:
+        with torch.cuda.device(device):
+            check(function(*args, torch._C._cuda_getCurrentRawStream(device.index)))
 
 
 class F8Weights:
     """A weight matrix [rows, cols] held as e4m3 values with a power of two per row and block of 128 columns."""
 
     def __init__(self, w):
-        lib = _lib.load()
         ld = _matrix("w", w)
         self.rows, self.cols = w.shape
         self.device = w.device
-        n = lib.onmt_f8_bytes(self.rows, self.cols)
-        self.buf = torch.empty(max(n, 1), dtype=torch.uint8, device=w.device)
-        with _device(w.device) as st:
-            check(lib.onmt_f8_pack(w.data_ptr(), _TYPES[w.dtype], ld, self.rows, self.cols, self.buf.data_ptr(), n, st))
+        n = _bytes_of("onmt_f8_bytes", self.rows, self.cols)
+        self.buf = torch.empty(n, dtype=torch.uint8, device=w.device)
+        _call(w.device, _lib.load().onmt_f8_pack, w.data_ptr(), _TYPES[w.dtype], ld, self.rows, self.cols, self.buf.data_ptr(), n)
 
     def values(self):
         """The fp32 values [rows, cols] that the weights stand for."""
-        lib = _lib.load()
         out = torch.empty(self.rows, self.cols, dtype=torch.float32, device=self.device)
-        with _device(self.device) as st:
-            check(lib.onmt_f8_unpack(self.buf.data_ptr(), self.buf.numel(), self.rows, self.cols, out.data_ptr(), self.cols,
-                                     st))
+        _call(self.device, _lib.load().onmt_f8_unpack, self.buf.data_ptr(), self.buf.numel(), self.rows, self.cols,
+              out.data_ptr(), self.cols)
         return out
 
     def linear(self, x, bias=None, out_dtype=torch.float32, out=None):
         """x [M, cols], rounded to 8 bits like the weights, times the weights' transpose, plus bias [rows] (fp32): [M, rows] of
         out_dtype, or written to out."""
-        lib = _lib.load()
-        ldx = _matrix("x", x, self.device, cols=self.cols)
+        device = self.device
+        ldx = _matrix("x", x, device, cols=self.cols)
         M = x.shape[0]
         if bias is not None:
-            _vector("bias", bias, self.rows, torch.float32, self.device)
+            _vector("bias", bias, self.rows, torch.float32, device)
         if out is None:
             if out_dtype not in _TYPES:
                 raise ValueError(f"out_dtype is {out_dtype}")
-            out = torch.empty(M, self.rows, dtype=out_dtype, device=self.device)
+            out = torch.empty(M, self.rows, dtype=out_dtype, device=device)
             ld = self.rows
         else:
-            ld = _matrix("out", out, self.device, M, self.rows)
-        n = lib.onmt_f8_linear_ws_bytes(M, self.cols)
-        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=self.device)
-        with _device(self.device) as st:
-            check(lib.onmt_f8_linear(x.data_ptr(), _TYPES[x.dtype], ldx, M, self.buf.data_ptr(), self.buf.numel(), self.rows,
-                                     self.cols, bias.data_ptr() if bias is not None else None, out.data_ptr(),
-                                     _TYPES[out.dtype], ld, ws.data_ptr(), n, st))
+            ld = _matrix("out", out, device, M, self.rows)
+        kind = _TYPES[out.dtype]
+        n = _bytes_of("onmt_f8_linear_ws_bytes", M, self.cols)
+        ws = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+        _call(device, _lib.load().onmt_f8_linear, x.data_ptr(), _TYPES[x.dtype], ldx, M, self.buf.data_ptr(), self.buf.numel(),
+              self.rows, self.cols, bias.data_ptr() if bias is not None else None, out.data_ptr(), kind, ld,
+              ws.data_ptr() if n else None, n)
         return out
 
 
@@ -170,7 +167,6 @@ def constrain(logits, rules=None, mode=0, K=1, out=None):
     """(out, ids, lse) of logits [N, V] under the rules (onmt_constrain). mode 0: out [N, V] fp32 log-probabilities; 1: out and
     ids [N, K] of the K largest; 2: out [N, V] = the logits under the rules, in their own type. What a mode does not give is None.
     out: where to write modes 0 and 2, the logits themselves for example."""
-    lib = _lib.load()
     ld = _matrix("logits", logits)
     N, V = logits.shape
     device = logits.device
@@ -185,24 +181,23 @@ def constrain(logits, rules=None, mode=0, K=1, out=None):
         if rules.words is not None and rules.words < (V + 31) // 32:
             raise ValueError(f"a mask of {rules.words} words does not cover {V} tokens")
         ref = ctypes.byref(rules.c)
-    cols = K if mode == 1 else V
+    out_dtype = logits.dtype if mode == 2 else torch.float32
     ids = lse = ws = None
     n = 0
     if out is not None:
         if mode == 1:
             raise ValueError("out is for modes 0 and 2")
-        ld_out = _matrix("out", out, device, N, V, (logits.dtype if mode == 2 else torch.float32,))
+        ld_out = _matrix("out", out, device, N, V, (out_dtype,))
     else:
-        out = torch.empty(N, max(cols, 0), dtype=logits.dtype if mode == 2 else torch.float32, device=device)
-        ld_out = cols
+        ld_out = K if mode == 1 else V
+        out = torch.empty(N, max(ld_out, 0), dtype=out_dtype, device=device)
     if mode != 2:
-        n = lib.onmt_constrain_ws_bytes(N, V, mode, K)
-        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+        n = _bytes_of("onmt_constrain_ws_bytes", N, V, mode, K)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
         lse = torch.empty(N, dtype=torch.float32, device=device)
         if mode == 1:
             ids = torch.empty(N, max(K, 0), dtype=torch.int32, device=device)
-    with _device(device) as st:
-        check(lib.onmt_constrain(ref, logits.data_ptr(), _TYPES[logits.dtype], ld, N, V, mode, K, out.data_ptr(), ld_out,
-                                 ids.data_ptr() if ids is not None else None, lse.data_ptr() if lse is not None else None,
-                                 ws.data_ptr() if ws is not None else None, n, st))
+    _call(device, _lib.load().onmt_constrain, ref, logits.data_ptr(), _TYPES[logits.dtype], ld, N, V, mode, K, out.data_ptr(),
+          ld_out, ids.data_ptr() if ids is not None else None, lse.data_ptr() if lse is not None else None,
+          ws.data_ptr() if n else None, n)
     return out, ids, lse

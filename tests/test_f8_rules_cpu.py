@@ -22,7 +22,7 @@ def test_sizes():
     for bad in ((0, 4), (4, 0), (-1, 4), (1 << 30, 1 << 10)):
         assert lib.onmt_f8_bytes(*bad) == 0
         assert lib.onmt_f8_linear_ws_bytes(*bad) == 0
-    assert lib.onmt_f8_linear_ws_bytes(5, 500) >= 5 * 500
+    assert lib.onmt_f8_linear_ws_bytes(100, 500) >= 100 * 500
     assert lib.onmt_constrain_ws_bytes(4, 1000, 2, 0) == 0
     assert lib.onmt_constrain_ws_bytes(4, 1000, 0, 0) > 0
     assert lib.onmt_constrain_ws_bytes(4, 1000, 1, 17) == 0
@@ -43,10 +43,10 @@ def linear(**kw):
     (dict(ldx=-500), _lib.ONMT_EINVAL), (dict(ldx=1 << 62), _lib.ONMT_EINVAL), (dict(M=0), _lib.ONMT_EINVAL),
     (dict(packed=None), _lib.ONMT_EINVAL), (dict(packed=W + 8), _lib.ONMT_EINVAL), (dict(pbytes=63 * 4 * 2048), _lib.ONMT_ESIZE),
     (dict(rows=0), _lib.ONMT_EINVAL), (dict(out=None), _lib.ONMT_EINVAL), (dict(ld_out=999), _lib.ONMT_EINVAL),
-    (dict(bias=P + 1), _lib.ONMT_EINVAL), (dict(ws=None), _lib.ONMT_EINVAL), (dict(ws=WS + 4), _lib.ONMT_EINVAL),
-    (dict(ws_bytes=64), _lib.ONMT_ESIZE),
+    (dict(bias=P + 1), _lib.ONMT_EINVAL), (dict(M=100, ws=None), _lib.ONMT_EINVAL), (dict(M=100, ws=WS + 4), _lib.ONMT_EINVAL),
+    (dict(M=100, ws_bytes=64), _lib.ONMT_ESIZE),
     # out over x, over the workspace, over the weights
-    (dict(out=P), _lib.ONMT_EINVAL), (dict(out=P + 5 * 500 * 4 - 4), _lib.ONMT_EINVAL), (dict(out=WS), _lib.ONMT_EINVAL),
+    (dict(out=P), _lib.ONMT_EINVAL), (dict(out=P + 5 * 500 * 4 - 4), _lib.ONMT_EINVAL), (dict(M=100, out=WS), _lib.ONMT_EINVAL),
     (dict(out=W + 64), _lib.ONMT_EINVAL),
     (dict(M=1 << 30, ldx=500), _lib.ONMT_EUNSUPPORTED),
 ])
