@@ -13,9 +13,11 @@
 //
 // Operands lie in fragment blocks of 16 rows x 128 columns, 2 KB: lane l of a wave holds row l % 16, columns 32 (l / 16) .. + 31,
 // its first 16 bytes at 16 l of the first kilobyte, the others at 16 l of the second. (The instruction's own order of the columns
-// does not matter as long as both operands have the same.) Consecutive blocks along the columns; then, behind all blocks,
-// the powers (biased by 127), one byte per row and block: the four blocks 4 j .. 4 j + 3 of a row are a dword, which the
-// instruction picks its byte from, the dwords of 16 rows side by side.
+// does not matter as long as both operands have the same.) Consecutive blocks go down the rows, so that what a tile of rows needs
+// of one block of columns is one stretch of memory (along the columns, the stretches of a tile lie a power of two apart for
+// many sizes and meet in few of the L2's channels: 8192-cubed took 467 us). Then, behind all blocks, the powers (biased
+// by 127), one byte per row and block: blocks 4 j .. 4 j + 3 of a row are a dword, which the instruction picks its byte
+// from, the dwords of all rows side by side, then those of the next four blocks.
 
 #include <type_traits>
 
@@ -91,7 +93,7 @@ template <class T>
 __global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_t ld, int rows, int cols, F8Mat out, int nblocks) {
   const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (b >= nblocks) return;
-  const int rb = b / out.kblocks, kb = b % out.kblocks;
+  const int rb = b % out.rblocks, kb = b / out.rblocks;
   const int r = rb * 16 + (lane & 15), g = lane >> 4;
   float v[32];
   load32(x + (int64_t)min(r, rows - 1) * ld, kb * kF8Block + 32 * g, r < rows ? cols : 0, v);
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_
   *(i32x4*)d = lo;
   *(i32x4*)(d + kF8Frag / 2) = hi;
   if (g == 0) {
-    uint8_t* s = (uint8_t*)(out.exps + ((size_t)rb * out.kquads() + kb / 4) * 16 + lane);
+    uint8_t* s = (uint8_t*)(out.exps + ((size_t)(kb / 4) * out.rblocks + rb) * 16 + lane);
     s[kb & 3] = (uint8_t)(kF8One + e);
     if (kb == out.kblocks - 1)
       for (int j = (kb & 3) + 1; j < 4; ++j) s[j] = kF8One;
@@ -115,9 +117,9 @@ __global__ __launch_bounds__(256) void k_f8_unpack(F8Mat w, int rows, int cols, 
   if (row >= rows) return;
   const int r = (int)row, c = (int)(i % quads) * 4;
   const int rb = r / 16, kb = c / kF8Block, g = c % kF8Block / 32, o = c % 32;
-  const int word = *(const int*)(w.data + ((size_t)rb * w.kblocks + kb) * kF8Frag + (o >= 16 ? kF8Frag / 2 : 0) +
+  const int word = *(const int*)(w.data + ((size_t)kb * w.rblocks + rb) * kF8Frag + (o >= 16 ? kF8Frag / 2 : 0) +
                                  (r % 16 + 16 * g) * 16 + o % 16);
-  const int e = (int)(((const uint8_t*)(w.exps + ((size_t)rb * w.kquads() + kb / 4) * 16 + r % 16))[kb & 3]) - kF8One;
+  const int e = (int)(((const uint8_t*)(w.exps + ((size_t)(kb / 4) * w.rblocks + rb) * 16 + r % 16))[kb & 3]) - kF8One;
   const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(word, 0), __builtin_amdgcn_cvt_f32_fp8(word, 1),
                       __builtin_amdgcn_cvt_f32_fp8(word, 2), __builtin_amdgcn_cvt_f32_fp8(word, 3)};
   for (int j = 0; j < 4 && c + j < cols; ++j) out[(int64_t)r * ld + c + j] = ldexpf(v[j], e);
@@ -207,29 +209,38 @@ __global__ __launch_bounds__(256) void k_f8_few(const X* __restrict__ x, int64_t
   constexpr bool EXACT = sizeof(T) == 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g = lane >> 4;
-  const int kb = w.kblocks, kq = w.kquads(), nrb = (N + 15) / 16;
+  const int kb = w.kblocks, kq = w.kquads(), nrb = w.rblocks;
   const int nb = min(blockIdx.x * 4 + wave, nrb - 1);
-  const char* wp = w.data + (size_t)nb * kb * kF8Frag + lane * 16;
-  const int* we = w.exps + (size_t)nb * kq * 16 + i16;
+  const char* wp = w.data + (size_t)nb * kF8Frag + lane * 16;
+  const int* we = w.exps + (size_t)nb * 16 + i16;
   i32x8 f[2][4];
   int ew[2];
   auto load = [&](int q, i32x8 (&r)[4], int& e) {
-    e = we[min(q, kq - 1) * 16];
+    e = we[(size_t)min(q, kq - 1) * nrb * 16];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = f8_frag(wp + (size_t)min(4 * q + j, kb - 1) * kF8Frag);
+    for (int j = 0; j < 4; ++j) r[j] = f8_frag(wp + (size_t)min(4 * q + j, kb - 1) * nrb * kF8Frag);
   };
   load(0, f[0], ew[0]);
   const f32x4 b4 = bias4(bias, N, nb * 16 + 4 * g);
-  // rows: fragment blocks [kb][TM], then the powers [TM][kq][16] as in a packed matrix
-  int* le = (int*)(lds + (size_t)kb * TM * kF8Frag);
+  // rows: fragment blocks [kb][TM], then the powers [TM][kq][16] as in a packed matrix; for fp32 results the values as bf16, each
+  // lane's four quarters in a kilobyte each (widened once here and not by every wave: 64 rows of 500 by 50000 28.7 us so)
+  constexpr int BLK = EXACT ? 2 * kF8Frag : kF8Frag;
+  int* le = (int*)(lds + (size_t)kb * TM * BLK);
   for (int b = wave; b < kb * TM; b += 4) {
     const int rb = b % TM, k = b / TM, r = rb * 16 + i16;
     float v[32];
     load32(x + (int64_t)min(r, M - 1) * ldx, k * kF8Block + 32 * g, r < M ? cols : 0, v);
     i32x4 lo, hi;
     const int e = f8_block(v, lo, hi);
-    *(i32x4*)(lds + (size_t)b * kF8Frag + lane * 16) = lo;
-    *(i32x4*)(lds + (size_t)b * kF8Frag + kF8Frag / 2 + lane * 16) = hi;
+    char* d = lds + (size_t)b * BLK + lane * 16;
+    if constexpr (EXACT) {
+      const Wide8 q = f8_widen(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), kF8One + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(bf16x8*)(d + i * 1024) = q.q[i];
+      continue;
+    }
+    *(i32x4*)d = lo;
+    *(i32x4*)(d + kF8Frag / 2) = hi;
     if (g == 0) ((uint8_t*)(le + (rb * kq + k / 4) * 16 + i16))[k & 3] = (uint8_t)(kF8One + e);
   }
   __syncthreads();
@@ -239,17 +250,27 @@ __global__ __launch_bounds__(256) void k_f8_few(const X* __restrict__ x, int64_t
   auto quad = [&](int q, const i32x8 (&r)[4], int e) {
     int ea[TM];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) ea[t] = le[(t * kq + q) * 16 + i16];
+    for (int t = 0; t < TM; ++t) ea[t] = EXACT ? 0 : le[(t * kq + q) * 16 + i16];
     auto step = [&](auto j) {
       constexpr int J = decltype(j)::value;
       const int k = 4 * q + J;
       if (k >= kb) return;
-      i32x8 a[TM];
+      const char* row = lds + (size_t)k * TM * BLK + lane * 16;
+      if constexpr (EXACT) {
+        const Wide8 b = f8_widen(r[J], e >> (8 * J) & 255);
 #pragma unroll
-      for (int t = 0; t < TM; ++t) a[t] = f8_frag(lds + (size_t)(k * TM + t) * kF8Frag + lane * 16);
-      const i32x8 b[1] = {r[J]};
-      const int eb[1] = {e};
-      f8_multiply<EXACT, J, TM, 1>(c, a, ea, b, eb);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int t = 0; t < TM; ++t)
+            c[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.q[i], *(const bf16x8*)(row + t * BLK + i * 1024), c[t][0], 0, 0, 0);
+      } else {
+        i32x8 a[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) a[t] = f8_frag(row + t * BLK);
+        const i32x8 b[1] = {r[J]};
+        const int eb[1] = {e};
+        f8_multiply<EXACT, J, TM, 1>(c, a, ea, b, eb);
+      }
     };
     step(Const<0>{});
     step(Const<1>{});
@@ -285,16 +306,37 @@ __global__ __launch_bounds__(256) void k_f8_few(const X* __restrict__ x, int64_t
   }
 }
 
+// A workgroup's tiles: bands of `band` row tiles, column tiles outer, so that what a band's rows and a few column tiles hold fits
+// an XCD's L2. Workgroups are dealt round-robin to the XCDs; each XCD has a contiguous range of tiles, which its
+// workgroups take in turn.
+struct F8Tiles {
+  int nm, nn, band, per, first, last;
+  __device__ __forceinline__ F8Tiles(int nm_, int nn_, int band_) : nm(nm_), nn(nn_), band(band_), per((int)gridDim.x / 8) {
+    const int n = nm * nn, xcd = blockIdx.x & 7;
+    first = xcd * (n / 8) + min(xcd, n % 8);
+    last = first + n / 8 + (xcd < n % 8 ? 1 : 0);
+  }
+  // The first row and column blocks of tile t.
+  __device__ __forceinline__ void at(int t, int rb, int cb, int& rb0, int& cb0) const {
+    const int b0 = t / (band * nn) * band, bh = min(band, nm - b0);
+    t -= b0 * nn;
+    rb0 = (b0 + t % bh) * rb;
+    cb0 = t / bh * cb;
+  }
+};
+
 // Many rows: 16 WM TM x 16 WN TN tiles of WM x WN waves, both operands through LDS in two stages of one 128-column block, moved
 // there by LDS-destination loads: a stage's loads are issued right behind the barrier that frees its buffer and are in flight
-// while the other stage is multiplied.
-template <int TM_, int TN_, int WM_, int WN_>
+// while the other stage is multiplied. A workgroup takes several tiles (SLOTS per 8 XCDs share them) and goes on to the next one's
+// first stage while it multiplies a tile's last, so that only the first tile waits for memory and a tile's stores drain
+// behind the next one's products (6400 x 1000 by 50000 fp16: 449 us with a workgroup per tile).
+template <int TM_, int TN_, int WM_, int WN_, int SLOTS_>
 struct F8Tile {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NT = 64 * WM * WN;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NT = 64 * WM * WN, SLOTS = SLOTS_;
   static constexpr int RB = WM * TM, CB = WN * TN, BM = 16 * RB, BN = 16 * CB;
-  static constexpr int STG = (RB + CB) * kF8Frag, LDS = 2 * STG;
+  static constexpr int STG = (RB + CB) * kF8Frag, EXP = 1024, LDS = 2 * STG + 4 * EXP;
   static constexpr int LPW = 2 * (RB + CB) / (WM * WN);          // 1 KB loads per wave and stage
-  static_assert(LPW * WM * WN == 2 * (RB + CB), "whole loads");
+  static_assert(LPW * WM * WN == 2 * (RB + CB) && RB <= 16 && CB <= 16, "whole loads");
 };
 
 template <class C, class T>
@@ -303,67 +345,94 @@ __global__ __launch_bounds__(C::NT) void k_f8_wide(F8Mat x, F8Mat w, int M, int 
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int TM = C::TM, TN = C::TN, W = C::WM * C::WN;
   __shared__ __attribute__((aligned(16))) char lds[C::LDS];
-  // tiles in bands of `band` row tiles, column tiles outer: what a band's rows and a few column tiles hold fits an XCD's L2
-  int t = xcd_remap(blockIdx.x, nm * nn);
-  const int b0 = t / (band * nn) * band, bh = min(band, nm - b0);
-  t -= b0 * nn;
-  const int rb0 = (b0 + t % bh) * C::RB, cb0 = t / bh * C::CB;
+  char* exps = lds + 2 * C::STG;                 // [four blocks' parity][rows, columns][16 blocks][16]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g = lane >> 4, wm = wave % C::WM, wn = wave / C::WM;
-  const int kb = x.kblocks, kq = x.kquads(), nrb = (M + 15) / 16, ncb = (N + 15) / 16;
+  const int kb = x.kblocks;
+
+  struct Where {
+    int rb0, cb0, nra, nca;
+  };
+  const F8Tiles tiles(nm, nn, band);
+  const int per = tiles.per, last = tiles.last;
+  auto where = [&](int t) {
+    Where p;
+    tiles.at(t, C::RB, C::CB, p.rb0, p.cb0);
+    p.nra = min(C::RB, x.rblocks - p.rb0);
+    p.nca = min(C::CB, w.rblocks - p.cb0);
+    return p;
+  };
 
   // load i of this wave moves half (w + W i) & 1 of block (w + W i) / 2 of the stage; row blocks past the operand's last
-  // re-read that (they are never stored)
-  const int nra = min(C::RB, nrb - rb0), nca = min(C::CB, ncb - cb0);
-  const uint32_t rowb = (uint32_t)kb * kF8Frag;
-  const __amdgpu_buffer_rsrc_t rx = make_rsrc(x.data + (size_t)rb0 * rowb, (uint32_t)nra * rowb);
-  const __amdgpu_buffer_rsrc_t rw = make_rsrc(w.data + (size_t)cb0 * rowb, (uint32_t)nca * rowb);
-  auto issue = [&](int st) {
-    char* base = lds + (st & 1) * C::STG;
+  // re-read that (they are never stored). Every fourth stage brings the powers of its block and the next three.
+  auto issue = [&](const Where& p, int st, int buf, int quad) {
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(x.data + ((size_t)st * x.rblocks + p.rb0) * kF8Frag, p.nra * kF8Frag);
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(w.data + ((size_t)st * w.rblocks + p.cb0) * kF8Frag, p.nca * kF8Frag);
+    char* base = lds + buf * C::STG;
 #pragma unroll
     for (int i = 0; i < C::LPW; ++i) {
       const int q = wave + W * i, b = q >> 1;
       const uint32_t half = (q & 1) * (kF8Frag / 2);
-      if (b < C::RB) dma16(rx, base + q * (kF8Frag / 2), (uint32_t)min(b, nra - 1) * rowb + half + lane * 16u, (uint32_t)st * kF8Frag);
-      else dma16(rw, base + q * (kF8Frag / 2), (uint32_t)min(b - C::RB, nca - 1) * rowb + half + lane * 16u, (uint32_t)st * kF8Frag);
+      if (b < C::RB) dma16(rx, base + q * (kF8Frag / 2), lane * 16u, (uint32_t)min(b, p.nra - 1) * kF8Frag + half);
+      else dma16(rw, base + q * (kF8Frag / 2), lane * 16u, (uint32_t)min(b - C::RB, p.nca - 1) * kF8Frag + half);
+    }
+    if ((st & 3) == 0 && wave < 2) {             // reads zeros past the tile's rows
+      const F8Mat& o = wave ? w : x;
+      const int b0 = wave ? p.cb0 : p.rb0, nb = wave ? p.nca : p.nra;
+      dma16(make_rsrc(o.exps + ((size_t)(st / 4) * o.rblocks + b0) * 16, nb * 64), exps + ((quad & 1) * 2 + wave) * C::EXP, lane * 16u, 0);
     }
   };
-  const int* xe[TM];
-  const int* we[TN];
-#pragma unroll
-  for (int a = 0; a < TM; ++a) xe[a] = x.exps + (size_t)min(rb0 + wm * TM + a, nrb - 1) * kq * 16 + i16;
-#pragma unroll
-  for (int a = 0; a < TN; ++a) we[a] = w.exps + (size_t)min(cb0 + wn * TN + a, ncb - 1) * kq * 16 + i16;
+  auto barrier = [&] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
-  f32x4 c[TM][TN];
+  int t = tiles.first + (int)(blockIdx.x >> 3);
+  if (t >= last) return;
+  Where at = where(t);
+  int buf = 0, quad = 0;
+  issue(at, 0, 0, 0);
+  __builtin_amdgcn_s_waitcnt(waitcnt_stage(0));
+  for (;;) {
+    const bool more = t + per < last;
+    const Where next = more ? where(t + per) : at;
+    f32x4 c[TM][TN];
 #pragma unroll
-  for (int a = 0; a < TM; ++a)
+    for (int a = 0; a < TM; ++a)
 #pragma unroll
-    for (int b = 0; b < TN; ++b) c[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  issue(0);
-  for (int q = 0; q < kq; ++q) {
-    int ea[TM], ew[TN];
+      for (int b = 0; b < TN; ++b) c[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int n0 = (at.cb0 + wn * TN) * 16;
+    int ea[TM], ew[TN];                            // powers of this block (low byte) and the next ones of its four
+    for (int st = 0; st < kb; ++st, buf ^= 1) {
+      // this wave's loads of stage st have landed (those of a tile's first stage before the stores of the tile before); behind
+      // the barrier everyone's have, and nobody reads the other buffer
+      if (st == 0) __builtin_amdgcn_s_waitcnt(waitcnt_stage(63));
+      else __builtin_amdgcn_s_waitcnt(waitcnt_stage(0));
+      barrier();
+      const bool wrap = st + 1 >= kb;
+      const int q = quad;
+      if (wrap || (st & 3) == 3) ++quad;
+      if (!wrap || more) issue(wrap ? next : at, wrap ? 0 : st + 1, buf ^ 1, quad);
+      if ((st & 3) == 0) {
+        const char* e = exps + (q & 1) * 2 * C::EXP + i16 * 4;
 #pragma unroll
-    for (int a = 0; a < TM; ++a) ea[a] = xe[a][q * 16];
+        for (int a = 0; a < TM; ++a) ea[a] = *(const int*)(e + (wm * TM + a) * 64);
 #pragma unroll
-    for (int a = 0; a < TN; ++a) ew[a] = we[a][q * 16];
-    auto step = [&](auto j) {
-      constexpr int J = decltype(j)::value;
-      const int st = 4 * q + J;
-      if (st >= kb) return;
-      // this wave's loads of stage st have landed; behind the barrier everyone's have, and nobody reads the other buffer
-      __builtin_amdgcn_s_waitcnt(waitcnt_stage(0));
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (st + 1 < kb) issue(st + 1);
-      const char* base = lds + (st & 1) * C::STG + lane * 16;
+        for (int b = 0; b < TN; ++b) ew[b] = *(const int*)(e + C::EXP + (wn * TN + b) * 64);
+      } else {
+#pragma unroll
+        for (int a = 0; a < TM; ++a) ea[a] >>= 8;
+#pragma unroll
+        for (int b = 0; b < TN; ++b) ew[b] >>= 8;
+      }
+      const char* base = lds + buf * C::STG + lane * 16;
       i32x8 wf[TN], af[TM];
 #pragma unroll
       for (int b = 0; b < TN; ++b) wf[b] = f8_frag(base + (C::RB + wn * TN + b) * kF8Frag);
 #pragma unroll
       for (int a = 0; a < TM; ++a) af[a] = f8_frag(base + (wm * TM + a) * kF8Frag);
-      f8_multiply<EXACT, J, TM, TN>(c, af, ea, wf, ew);
+      f8_multiply<EXACT, 0, TM, TN>(c, af, ea, wf, ew);
       if constexpr (!EXACT) {       // rows' fragments one ahead of the products that take them
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * TN + 4, 0);
 #pragma unroll
@@ -372,53 +441,58 @@ __global__ __launch_bounds__(C::NT) void k_f8_wide(F8Mat x, F8Mat w, int M, int 
           __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
       }
-    };
-    step(Const<0>{});
-    step(Const<1>{});
-    step(Const<2>{});
-    step(Const<3>{});
-  }
-  // the wave's 16 TM x 64 results through LDS, 16 bytes of a row per lane: whole 128-byte lines leave, where the accumulators'
-  // own layout has 8 or 16 bytes of 16 rows per store. Chunks of a row are swizzled by the row against bank conflicts.
-  constexpr int VEC = kVec<T>, CH = 16 * TN / VEC, RPI = kWave / CH;      // chunks per row, rows per store
-  static_assert(TN == 4 && W * 16 * TM * CH * 16 <= C::LDS, "a wave's results fit its part of LDS");
-  const int m0 = (rb0 + wm * TM) * 16, n0 = (cb0 + wn * TN) * 16;
-  f32x4 add[TN];
-#pragma unroll
-  for (int b = 0; b < TN; ++b) add[b] = bias4(bias, N, n0 + 16 * b + 4 * g);
-  __builtin_amdgcn_s_waitcnt(waitcnt_stage(63));
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  char* mine = lds + wave * (16 * TM * CH * 16);
-#pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int b = 0; b < TN; ++b) {
-      const f32x4 v = c[a][b] + add[b];
-      T o[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = from_float<T>(v[j]);
-      const int r = 16 * a + i16, k = 16 * b + 4 * g;
-      __builtin_memcpy(__builtin_assume_aligned(mine + (r * CH + ((k / VEC) ^ (r & (CH - 1)))) * 16 + k % VEC * (int)sizeof(T), 4 * sizeof(T)), o, 4 * sizeof(T));
     }
-  __builtin_amdgcn_wave_barrier();
-  const int rl = lane / CH, n = n0 + lane % CH * VEC;
-#pragma unroll 4
-  for (int it = 0; it < 16 * TM / RPI; ++it) {
-    const int r = it * RPI + rl, m = m0 + r;
-    typedef T vec __attribute__((ext_vector_type(VEC)));
-    const vec v = *(const vec*)(mine + (r * CH + ((lane % CH) ^ (r & (CH - 1)))) * 16);
-    if (m < M) {
-      T* p = out + (int64_t)m * ld + n;
-      if (n + VEC <= N) {
-        *(typename Packed<T, VEC>::type*)p = v;
-      } else {
+    // The tile's results through the buffer that was multiplied last, half of every wave's rows at a time: 256 or 512 bytes of a row leave
+    // together, where the accumulators' own layout has 8 or 16 bytes of 16 rows per store. Chunks of 16 bytes are swizzled by
+    // the row against bank conflicts. The next tile's first stage is waited for here, so that nothing has to wait for the stores.
+    constexpr int VEC = kVec<T>, CH = C::BN / VEC, RPI = kWave / CH;      // chunks per row, rows per store
+    constexpr int ROWS = C::BM / 2;                                       // per pass
+    static_assert(TN == 4 && ROWS * CH * 16 <= C::STG && ROWS % (RPI * W) == 0, "half a tile in a buffer");
+    f32x4 add[TN];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          if (n + j < N) p[j] = v[j];
+    for (int b = 0; b < TN; ++b) add[b] = bias4(bias, N, n0 + 16 * b + 4 * g);
+    __builtin_amdgcn_s_waitcnt(waitcnt_stage(0));
+    char* mid = lds + (buf ^ 1) * C::STG;
+    const int n = at.cb0 * 16 + lane % CH * VEC;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_stage(63));
+      barrier();
+#pragma unroll
+      for (int a = 0; a < TM / 2; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b) {
+          const f32x4 v = c[pass * (TM / 2) + a][b] + add[b];
+          typedef T quarter __attribute__((ext_vector_type(4)));
+          quarter o;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = from_float<T>(v[j]);
+          const int r = wm * (8 * TM) + 16 * a + i16, k = wn * 64 + 16 * b + 4 * g;
+          *(quarter*)(mid + (r * CH + ((k / VEC) ^ (r & 7))) * 16 + k % VEC * (int)sizeof(T)) = o;
+        }
+      __builtin_amdgcn_s_waitcnt(waitcnt_stage(63));
+      barrier();
+#pragma unroll
+      for (int it = 0; it < ROWS / RPI / W; ++it) {
+        const int r = (it * W + wave) * RPI + lane / CH;
+        const int m = at.rb0 * 16 + r / (8 * TM) * (16 * TM) + pass * (8 * TM) + r % (8 * TM);
+        typedef T vec __attribute__((ext_vector_type(VEC)));
+        const vec v = *(const vec*)(mid + (r * CH + ((lane % CH) ^ (r & 7))) * 16);
+        if (m < M) {
+          T* p = out + (int64_t)m * ld + n;
+          if (n + VEC <= N) {
+            __builtin_nontemporal_store((typename Packed<T, VEC>::type)v, (typename Packed<T, VEC>::type*)p);
+          } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+              if (n + j < N) p[j] = v[j];
+          }
+        }
       }
     }
+    if (!more) return;
+    t += per;
+    at = next;
   }
 }
 
@@ -447,17 +521,22 @@ hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld,
   return hipGetLastError();
 }
 
-// Rows whose 8-bit values a workgroup of k_f8_few holds in LDS beside their powers: 16, 32 or 64 of them, 0 if they are too many.
-constexpr int kFewLds = 64 << 10;
-static int few_rows(int M, int cols) {
+// LDS of a workgroup of k_f8_few for 16 tm rows, and the row tiles that it takes: 1, 2 or 4, 0 if the rows are too many for it. It is
+// level with the wide tiles or ahead of them wherever it can run (us, few against wide: 16 x 500 by 50000 fp32 8.5 and
+// 15.9, 64 rows 17.1 and 17.1, 17 x 1000 by 50000 fp32 23.2 and 22.7, 64 x 1024 by 32000 bf16 13.3 and 13.4, 16 x 64 by 1000 4.7 and 8.9).
+constexpr size_t kFewLds = 64 << 10;
+static size_t few_lds(int tm, int cols, bool exact) {
+  return (exact ? 2 : 1) * f8_data_bytes(16 * tm, cols) + f8_exp_bytes(16 * tm, cols);
+}
+static int few_rows(int M, int cols, bool exact) {
   const int tm = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-  return M <= 64 && f8_data_bytes(16 * tm, cols) + f8_exp_bytes(16 * tm, cols) <= kFewLds ? tm : 0;
+  return M <= 64 && few_lds(tm, cols, exact) <= kFewLds ? tm : 0;
 }
 
 template <class X, class T, int TM>
 static void launch_few(const void* x, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out, int64_t ld,
                        hipStream_t st) {
-  const int bytes = (int)(f8_data_bytes(16 * TM, cols) + f8_exp_bytes(16 * TM, cols));
+  const int bytes = (int)few_lds(TM, cols, sizeof(T) == 4);
   hipLaunchKernelGGL((k_f8_few<X, T, TM>), dim3((N + 63) / 64), dim3(256), bytes, st, (const X*)x, ldx, w, M, N, cols, bias,
                      (T*)out, ld);
 }
@@ -465,14 +544,15 @@ static void launch_few(const void* x, int64_t ldx, int M, const F8Mat& w, int N,
 template <class C, class T>
 static void launch_wide(const F8Mat& x, int M, const F8Mat& w, int N, const float* bias, void* out, int64_t ld, hipStream_t st) {
   const int nm = (M + C::BM - 1) / C::BM, nn = (N + C::BN - 1) / C::BN;
-  hipLaunchKernelGGL((k_f8_wide<C, T>), dim3(nm * nn), dim3(C::NT), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nn, 8);
+  const int slots = min(C::SLOTS, (nm * nn + 7) / 8 * 8);         // whole rounds of the XCDs
+  hipLaunchKernelGGL((k_f8_wide<C, T>), dim3(slots), dim3(C::NT), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nn, 8);
 }
 
-size_t f8_linear_ws(int M, int cols) { return few_rows(M, cols) ? 0 : f8_data_bytes(M, cols) + f8_exp_bytes(M, cols); }
+size_t f8_linear_ws(int M, int cols) { return few_rows(M, cols, true) ? 0 : f8_data_bytes(M, cols) + f8_exp_bytes(M, cols); }
 
 hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out,
                      int out_dtype, int64_t ld, void* ws, hipStream_t st) {
-  if (const int tm = few_rows(M, cols))
+  if (const int tm = few_rows(M, cols, out_dtype == kF32))
     return f8_type(dtype, [&](auto* tx) {
       f8_type(out_dtype, [&](auto* to) {
         using X = ONMT_TYPE(tx);
@@ -483,11 +563,14 @@ hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& 
   const F8Mat xm = f8_mat(ws, M, cols);
   const hipError_t e = f8_pack(x, dtype, ldx, M, cols, xm, st);
   if (e != hipSuccess) return e;
+  // 128 x 128 tiles, two workgroups per CU; 256 x 256 for 16-bit results of many rows, whose 8-bit products would else wait for LDS
+  // (256 x 500 by 50000 fp16 24 us with the small tiles, 22 with the large; 20480 x 1024 by 4096 bf16 119 and 106; 128 rows of
+  // 500 by 50000 bf16 14.4 and 18)
   return f8_type(out_dtype, [&](auto* to) {
     using T = ONMT_TYPE(to);
     if constexpr (sizeof(T) == 2)
-      if (M > 256) return launch_wide<F8Tile<8, 4, 2, 4>, T>(xm, M, w, N, bias, out, ld, st);
-    launch_wide<F8Tile<4, 4, 2, 2>, T>(xm, M, w, N, bias, out, ld, st);
+      if (M > 192) return launch_wide<F8Tile<8, 4, 2, 4, 256>, T>(xm, M, w, N, bias, out, ld, st);
+    launch_wide<F8Tile<4, 4, 2, 2, 512>, T>(xm, M, w, N, bias, out, ld, st);
   });
 }
 

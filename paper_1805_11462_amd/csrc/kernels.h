@@ -273,7 +273,7 @@ constexpr int kF8Frag = 16 * kF8Block;         // bytes of a fragment block
 struct F8Mat {
   char* data;
   int* exps;
-  int kblocks;
+  int rblocks, kblocks;
   __host__ __device__ int kquads() const { return (kblocks + 3) / 4; }
 };
 // Bytes of the fragment blocks and of the powers behind them.
@@ -284,7 +284,7 @@ inline size_t f8_exp_bytes(int64_t rows, int cols) {
   return (size_t)((rows + 15) / 16) * (((cols + kF8Block - 1) / kF8Block + 3) / 4) * 64;
 }
 inline F8Mat f8_mat(void* buf, int64_t rows, int cols) {
-  return F8Mat{(char*)buf, (int*)((char*)buf + f8_data_bytes(rows, cols)), (cols + kF8Block - 1) / kF8Block};
+  return F8Mat{(char*)buf, (int*)((char*)buf + f8_data_bytes(rows, cols)), (int)((rows + 15) / 16), (cols + kF8Block - 1) / kF8Block};
 }
 hipError_t f8_pack(const void* x, int dtype, int64_t ld, int rows, int cols, const F8Mat& out, hipStream_t st);
 hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld, hipStream_t st);
