@@ -295,6 +295,13 @@ size_t onmt_f8_linear_ws_bytes(int M, int cols);
 int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* packed, size_t packed_bytes, int rows, int cols,
                    const float* bias, void* out, int out_dtype, int64_t ld_out, void* ws, size_t ws_bytes, void* stream);
 
+/* The model's own steps with an 8-bit generator: packed = onmt_f8_pack of W_s [tgt_vocab, hidden] (fp32 or bf16 models; on the
+ * model's GPU; it stays allocated while it is set), NULL for the model's own weights again. From then on onmt_decode_step and
+ * onmt_beam_search compute the logits from the attentional vectors by onmt_f8_linear (fp32 results, the model's b_s) and everything
+ * else as before. Workspace sizes change with it: ask for them afterwards. B * beam rows of logits may take 16 GiB
+ * (ONMT_EUNSUPPORTED beyond); onmt_decode_step_noalloc and onmt_score refuse with ONMT_EUNSUPPORTED while it is set. */
+int onmt_set_generator(onmt_model* model, const void* packed, size_t packed_bytes);
+
 /* ---- Rules on logits ----------------------------------------------------------------------------------
  * For step loops outside the library: penalties for repeated tokens, biases, bans of repeated n-grams and grammar masks on logits
  * [N, V] (those of onmt_decode_step in mode 2, of onmt_f8_linear, or others), then the decoder step's modes. With x the logit of

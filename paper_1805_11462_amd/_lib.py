@@ -76,6 +76,7 @@ SIGNATURES = {
     "onmt_f8_linear_ws_bytes": (c_size_t, [c_int, c_int]),
     "onmt_f8_linear": (c_int, [c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_int, c_int, c_void_p, c_void_p,
                                c_int, c_int64, c_void_p, c_size_t, c_void_p]),
+    "onmt_set_generator": (c_int, [c_void_p, c_void_p, c_size_t]),
     "onmt_constrain_ws_bytes": (c_size_t, [c_int, c_int, c_int, c_int]),
     "onmt_constrain": (c_int, [POINTER(OnmtLogitRules), c_void_p, c_int, c_int64, c_int, c_int, c_int, c_int, c_void_p,
                                c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),

@@ -9,6 +9,67 @@
 
 namespace onmt {
 
+// ------------------------------------------------------------------ partials of given logits
+// Half a wave per (row, 128-column tile), four logits per lane: the tile's largest logit, the sum of exp(logit - that) and
+// the largest that the filters allow, as the generator's epilogue leaves them. Bound by memory (320 x 50000: 64 MB).
+__device__ inline float half_max(float v) {
+  v = fmaxf(v, dpp_move<0x111, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x112, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x114, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x118, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x142, 0xa>(v, v));
+  return (threadIdx.x & 32) ? readlane_f(v, 63) : readlane_f(v, 31);
+}
+
+__global__ __launch_bounds__(256) void k_tile_partials(GenParams p, int M, int pairs) {
+  typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const float ninf = -__builtin_inff();
+  for (int row = blockIdx.y * 4 + wave; row < M; row += gridDim.y * 4) {
+    const bool unk = p.pfmax && p.unk_cnt && p.max_unk >= 0 && p.unk_cnt[row] >= p.max_unk;
+    const float* x = p.logits + (size_t)row * p.ld_logits;
+    for (int i = blockIdx.x; i < pairs; i += gridDim.x) {
+      const int t = 2 * i + (lane >> 5), c = t * 128 + 4 * (lane & 31);
+      float v[4];
+      if (c + 4 <= p.V) {
+        const f32x4_a4 q = *(const f32x4_a4*)(x + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = q[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = c + j < p.V ? x[c + j] : ninf;
+      }
+      const float mx = half_max(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += mx > ninf ? __expf(v[j] - mx) : 0.f;
+      s = group_sum<32>(s);
+      float fx = ninf;
+      if (p.pfmax) {
+        const uint32_t out = p.banned_bits && c < p.V ? p.banned_bits[c >> 5] >> (c & 31) : 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (!(out >> j & 1) && !(unk && c + j == p.unk_id)) fx = fmaxf(fx, v[j]);
+        fx = half_max(fx);
+      }
+      if ((lane & 31) == 31 && t < p.ntiles) {
+        const size_t o = (size_t)row * p.ntiles + t;
+        p.pmax[o] = mx;
+        p.psum[o] = s;
+        if (p.pfmax) p.pfmax[o] = fx;
+      }
+    }
+  }
+}
+
+hipError_t tile_partials(const GenParams& p, int M, hipStream_t st) {
+  const int pairs = (p.ntiles + 1) / 2, rows = (M + 3) / 4 < 65535 ? (M + 3) / 4 : 65535;
+  // a wave takes a few pairs of tiles of its row; at most some thousands of workgroups
+  const int per = pairs * (int64_t)rows > 16384 ? 8 : 1;
+  hipLaunchKernelGGL(k_tile_partials, dim3((pairs + per - 1) / per, rows), dim3(256), 0, st, p, M, pairs);
+  return hipGetLastError();
+}
+
 // ------------------------------------------------------------------ softmax merge
 // One wave merges one row's generator partials (per column tile: max, sum of exp) and logits into the row's
 // logsumexp and top-K (larger logit first, smaller id on ties).

@@ -201,6 +201,8 @@ struct GenPartials {
   int unk_id, max_unk;
 };
 
+// The generator's partials (p.pmax, p.psum, with filters p.pfmax) of M rows of logits that another product left in p.logits.
+hipError_t tile_partials(const GenParams& p, int M, hipStream_t st);
 hipError_t lse_topk_merge(const GenPartials& gp, int M, int K, float* out_val, int32_t* out_id, float* out_lse,
                           hipStream_t st);
 // Teacher-forced scoring of all steps: rows r = t * B + b of the generator partials; logp[b * ld + t] =

@@ -71,6 +71,7 @@ struct Dims {
   bool bf16;
   int esz;             // operand element size
   int attn;            // ONMT_ATTN_GENERAL / _DOT / _CONCAT
+  bool gen8 = false;   // the generator is a caller's 8-bit matrix: workspaces hold logits at every beam width, and its scratch
   // fp16 terms per weight of the two-term products (split16.h): bf16 weights fit one, fp32 weights take two
   int wterms;
   // columns as the model-size refusals count them
@@ -201,6 +202,7 @@ struct onmt_model {
   Split16 W_s{};                           // the generator's weights: ceil128(Vt) rows of wterms fp16 terms
   const int32_t* W_s_exp = nullptr;        // power of two that undoes a vocabulary column's operand scales
   const float* b_s = nullptr;
+  const void* W_8 = nullptr;               // with d.gen8: the generator's weights in 8 bits, the caller's (onmt_f8_pack)
   // decoder layer 0's input-projection rows for every target token, E_tgt[v] W_e^T in the packed (gate-
   // blocked) column order, fp32 [Vt, 4 H_pad]; computed on the device when the model is created
   float* emb_gates = nullptr;
@@ -704,6 +706,7 @@ struct StepWs {
   float* pfmax;    // [N, ntiles] largest allowed logit per tile (hypothesis filters)
   int32_t* tok_s;  // [N] previous tokens and parents checked on the device (device validation)
   int32_t* par_s;
+  char* act8;      // scratch of the 8-bit generator
   int ntiles;
   int ld_logits;
 };
@@ -725,7 +728,7 @@ size_t step_layout(const Dims& d, int B, int S, int K, char* base, StepWs* w, bo
   t.pmax = c.take<float>(N * t.ntiles);
   t.psum = c.take<float>(N * t.ntiles);
   t.ld_logits = t.ntiles * gen_tile_cols();
-  lists = lists || K == 1 || N * t.ld_logits * sizeof(float) > kMaxLogitsBytes;
+  lists = !d.gen8 && (lists || K == 1 || N * t.ld_logits * sizeof(float) > kMaxLogitsBytes);
   t.logits = lists ? nullptr : c.take<float>(N * t.ld_logits);
   t.pval = lists ? c.take<float>(N * t.ntiles * K) : nullptr;
   t.pid = lists ? c.take<int32_t>(N * t.ntiles * K) : nullptr;
@@ -734,6 +737,7 @@ size_t step_layout(const Dims& d, int B, int S, int K, char* base, StepWs* w, bo
   t.pfmax = c.take<float>(N * t.ntiles);
   t.tok_s = c.take<int32_t>(N);
   t.par_s = c.take<int32_t>(N);
+  t.act8 = c.take<char>(d.gen8 ? f8_linear_ws((int)N, d.H) : 0);
   if (w) *w = t;
   return align_up(c.off);
 }
@@ -1228,7 +1232,13 @@ int decode_compute(onmt_model* m, const EncWs& w, int B, int S, int K, const Sta
     gp.pfmax = ex.pfmax;
     part = gen_partials(gp);
     if (timing) time_begin(m, st);
-    HIP_TRY(gemm_gen(Split16{out.feed16, N, d.kb(d.H)}, m->W_s, d.wterms, gp, st));
+    if (d.gen8) {
+      HIP_TRY(f8_linear(out.feed, kF32, d.H, N, f8_mat((void*)m->W_8, d.Vt, d.H), d.Vt, d.H, m->b_s, gp.logits, kF32, gp.ld_logits,
+                        sw.act8, st));
+      if (mode != 4) HIP_TRY(tile_partials(gp, N, st));
+    } else {
+      HIP_TRY(gemm_gen(Split16{out.feed16, N, d.kb(d.H)}, m->W_s, d.wterms, gp, st));
+    }
     if (timing) time_end(m, st);
   }
   if (mode == 2 || mode == 4) return ONMT_OK;
@@ -1238,6 +1248,14 @@ int decode_compute(onmt_model* m, const EncWs& w, int B, int S, int K, const Sta
   } else {
     HIP_TRY(lse_topk_merge(part, N, K, logp, ids, lse_out, st));
   }
+  return ONMT_OK;
+}
+
+// The 8-bit generator has no top-K lists to fall back to.
+int check_gen8(const onmt_model* m, long long B, long long K) {
+  const uint64_t row = (uint64_t)ceil_to(m->d.Vt, gen_tile_cols()) * sizeof(float);
+  if (m->d.gen8 && (uint64_t)(B * K) * row > kMaxLogitsBytes)
+    return fail(ONMT_EUNSUPPORTED, "B * beam = %lld rows of logits pass 16 GiB: too many for the 8-bit generator", B * K);
   return ONMT_OK;
 }
 
@@ -1365,6 +1383,7 @@ int onmt_decode_step(onmt_model* m, const void* enc_ws, int B, int S, int K, con
   int rc = check_beam(m, S, K);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, K, 0))) return rc;
+  if ((rc = check_gen8(m, B, K))) return rc;
   if (mode < 0 || mode > 2) return fail(ONMT_EINVAL, "mode must be 0 (full), 1 (top-K) or 2 (logits)");
   if (mode == 2 && lse) return fail(ONMT_EINVAL, "lse must be NULL in mode 2");
   if (mode == 1 && !ids) return fail(ONMT_EINVAL, "ids is NULL in top-K mode");
@@ -1425,6 +1444,7 @@ int onmt_decode_step_noalloc(onmt_model* m, const void* enc_ws, int B, int S, in
   int rc = check_beam(m, S, K);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, K, 0))) return rc;
+  if (m->d.gen8) return fail(ONMT_EUNSUPPORTED, "the allocation-free step has no room for an 8-bit generator's logits");
   if (mode < 0 || mode > 2) return fail(ONMT_EINVAL, "mode must be 0 (full), 1 (top-K) or 2 (logits)");
   if (mode == 2 && lse) return fail(ONMT_EINVAL, "lse must be NULL in mode 2");
   if (mode == 1 && !ids) return fail(ONMT_EINVAL, "ids is NULL in top-K mode");
@@ -1491,6 +1511,7 @@ int onmt_beam_search(onmt_model* m, const int32_t* src, const int32_t* len, int 
   int rc = check_beam(m, S, K);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, K, 0))) return rc;
+  if ((rc = check_gen8(m, B, K))) return rc;
   if (ws_bytes < search_layout(m->d, B, S, K, T, nullptr, nullptr)) return fail(ONMT_ESIZE, "search workspace too small");
   hipStream_t st = (hipStream_t)stream;
   SearchWs w;
@@ -1615,6 +1636,7 @@ int onmt_score(onmt_model* m, const int32_t* src, const int32_t* len, int B, int
   if (!out_logp || !out_nll) return fail(ONMT_EINVAL, "NULL output pointer");
   if (B < 1 || S < 1) return fail(ONMT_EINVAL, "B and S_max must be >= 1");
   if (T < 1 || T > 100000) return fail(ONMT_EINVAL, "T_max %d outside [1, 100000]", T);
+  if (m->d.gen8) return fail(ONMT_EUNSUPPORTED, "scoring keeps no logits for an 8-bit generator (onmt_set_generator(model, NULL, 0))");
   int rc = check_beam(m, S, 1);
   if (rc) return rc;
   if ((rc = check_ws_limits(m->d, B, S, 1, T))) return rc;
@@ -1730,6 +1752,17 @@ int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* pac
     return fail(ONMT_EINVAL, "out overlaps x, ws or packed");
   hipStream_t st = (hipStream_t)stream;
   HIP_TRY(f8_linear(x, dtype, ldx, M, f8_mat((void*)packed, rows, cols), rows, cols, bias, out, out_dtype, ld_out, ws, st));
+  return ONMT_OK;
+}
+
+int onmt_set_generator(onmt_model* m, const void* packed, size_t packed_bytes) {
+  if (!m) return fail(ONMT_EINVAL, "model is NULL");
+  if (packed) {
+    const int rc = check_packed(packed, packed_bytes, m->cfg.tgt_vocab, m->cfg.hidden);
+    if (rc) return rc;
+  }
+  m->W_8 = packed;
+  m->d.gen8 = packed != nullptr;
   return ONMT_OK;
 }
 

@@ -145,6 +145,18 @@ class Translator:
                                         _ptr(attn), _ptr(ws), n, _stream()))
         return out_state, logp, ids, lse, attn
 
+    def set_generator(self, weights=None):
+        """Steps and searches with an 8-bit generator: weights = ops.F8Weights of W_s [tgt_vocab, hidden], None for the model's
+        own again. Buffers of searches are to be allocated afterwards."""
+        if weights is not None:
+            if (weights.rows, weights.cols) != (self.cfg.tgt_vocab, self.cfg.hidden):
+                raise ValueError(f"the generator is [{self.cfg.tgt_vocab}, {self.cfg.hidden}], got [{weights.rows}, {weights.cols}]")
+            if weights.device != self.wbuf.device:
+                raise ValueError(f"the model is on {self.wbuf.device}, the weights on {weights.device}")
+        check(self.lib.onmt_set_generator(self.handle, _ptr(weights.buf) if weights is not None else None,
+                                          weights.buf.numel() if weights is not None else 0))
+        self.generator = weights                    # kept alive while it is set
+
     # ---------------------------------------------------------------- search
     def search_buffers(self, B, S, beam, max_len, alpha=0.0, check_every=0, trace=False, beta=0.0, max_unk=-1,
                        banned=(), align=False):

@@ -55,6 +55,11 @@ def test_linear_refusals(kw, code):
     assert len(_lib.load().onmt_last_error()) > 0
 
 
+def test_generator_needs_a_model():
+    assert _lib.load().onmt_set_generator(None, P, 1 << 30) == _lib.ONMT_EINVAL
+    assert _lib.load().onmt_set_generator(None, None, 0) == _lib.ONMT_EINVAL
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(w=None), _lib.ONMT_EINVAL), (dict(dtype=9), _lib.ONMT_EINVAL), (dict(ld=3), _lib.ONMT_EINVAL),
     (dict(nbytes=100), _lib.ONMT_ESIZE), (dict(packed=None), _lib.ONMT_EINVAL), (dict(rows=1 << 28, nbytes=1 << 62), _lib.ONMT_EUNSUPPORTED),

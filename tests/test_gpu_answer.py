@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import workloads as W
-from paper_1805_11462_amd import ops
+from paper_1805_11462_amd import _lib, ops
 from tests._gpu import translator_for
+from tests.test_gpu_f8 import round8
 
 pytestmark = pytest.mark.gpu
 
@@ -87,4 +88,140 @@ def test_a_greedy_loop_with_rules():
         history[:, t] = tok
         n += 1
     assert all(len(set(s)) == T for s in said)
+    tr.close()
+
+
+def _log_softmax(y):
+    top = y.max(axis=1, keepdims=True)
+    return y - (top + np.log(np.exp(y - top).sum(axis=1, keepdims=True)))
+
+
+def _model(wdtype="fp32", **kw):
+    w = W.Workload(**{**W.get("tiny").as_dict(), "hidden": 136, "emb": 40, "tgt_vocab": 1500, "wdtype": wdtype, **kw})
+    weights = W.make_weights(w, peaked=True)
+    tr = translator_for(w, weights)
+    return w, weights, tr, ops.F8Weights(torch.from_numpy(weights["W_s"]).cuda())
+
+
+@pytest.mark.parametrize("wdtype,K,B", [("fp32", 3, 4), ("bf16", 1, 4), ("fp32", 5, 40)])
+def test_steps_with_an_8_bit_generator(wdtype, K, B):
+    """Every mode of a step against the definition in 64 bits on the step's own attentional vectors. Tolerance: sums of 136 exact
+    products in fp32 (137 x 2^-24 of the products' sizes), then the softmax's 2^-18."""
+    w, weights, tr, w8 = _model(wdtype, batch=B)
+    src, lens = W.make_batch(w)
+    S, N = src.shape[1], B * K
+    ws = tr.encode(torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda())
+    st = tr.decode_init(ws, B, S, K)
+    tok = torch.full((N,), W.BOS_ID, dtype=torch.int32, device="cuda")
+    own = tr.decode_step(ws, B, S, K, st, tok, mode=0)
+    tr.set_generator(w8)
+    full, top, raw = (tr.decode_step(ws, B, S, K, st, tok, mode=m) for m in (0, 1, 2))
+    for other in (full, top, raw):
+        for a, b in zip(tr.state_views(own[0], N), tr.state_views(other[0], N)):
+            assert torch.equal(a, b)
+    feed = round8(tr.state_views(raw[0], N)[2].cpu().numpy())
+    wq = round8(weights["W_s"])
+    y = feed @ wq.T + weights["b_s"].astype(np.float64)
+    tol = (w.hidden + 1) * 2.0 ** -24 * (np.abs(feed) @ np.abs(wq).T) + 2.0 ** -24 * np.abs(y)
+    assert (np.abs(raw[1].double().cpu().numpy() - y) <= tol).all()
+    ref = _log_softmax(y)
+    assert (np.abs(full[1].double().cpu().numpy() - ref) <= 2 * tol.max(axis=1, keepdims=True) + 2.0 ** -18 * (1 + np.abs(ref))).all()
+    order = torch.sort(raw[1], dim=1, descending=True, stable=True)
+    assert torch.equal(top[2], order.indices[:, :K].to(torch.int32))
+    assert (top[1] - full[1].gather(1, order.indices[:, :K])).abs().max() <= 2.0 ** -18 * (1 + full[1].abs().max())
+    tr.set_generator(None)
+    again = tr.decode_step(ws, B, S, K, st, tok, mode=0)
+    assert torch.equal(again[1], own[1])
+    tr.close()
+
+
+@pytest.mark.parametrize("beam,banned", [(1, ()), (4, ()), (3, (5, 17, 200))])
+def test_searches_with_an_8_bit_generator(beam, banned):
+    """A search is the external loop over steps: the same sums of log-probabilities, the same choices."""
+    w, weights, tr, w8 = _model()
+    tr.set_generator(w8)
+    src, lens = W.make_batch(w)
+    src_d, lens_d = torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda()
+    B, S = src.shape
+    T = 6
+    buf = tr.search_buffers(B, S, beam, T, trace=True, banned=banned)
+    tr.beam_search(src_d, lens_d, buf)
+    slot, tok, cand = (buf[f"trace_{k}"].cpu().numpy() for k in ("slot", "tok", "cand"))
+    steps = buf["trace_steps"].cpu().numpy()
+    ws = tr.encode(src_d, lens_d)
+    st = tr.decode_init(ws, B, S, beam)
+    score = np.full((B, beam), -np.inf)
+    score[:, 0] = 0.0
+    prev = np.full((B, beam), W.BOS_ID)
+    parent = None
+    live = np.ones(B, bool)
+    for t in range(T):
+        st, logp, _, _, _ = tr.decode_step(ws, B, S, beam, st, torch.from_numpy(prev.reshape(-1).astype(np.int32)).cuda(), parent,
+                                           mode=0)
+        lp = logp.double().cpu().numpy().reshape(B, beam, -1)
+        lp[:, :, list(banned)] = -np.inf
+        both = score[:, :, None] + lp
+        nparent = np.tile(np.arange(beam), (B, 1))
+        for b in range(B):
+            live[b] &= t < steps[b]
+            if not live[b]:
+                continue
+            flat = np.argsort(-both[b].reshape(-1), kind="stable")[:beam]
+            # the step's own fp32 log-probabilities: both sides add the same numbers but for the softmax's last bits
+            assert np.allclose(cand[t, b], both[b].reshape(-1)[flat], rtol=0, atol=2.0 ** -17 * (t + 1) * 20)
+            assert (tok[t, b] == flat % w.tgt_vocab).all() and (slot[t, b] == flat // w.tgt_vocab).all()
+            n = 0
+            score[b] = -np.inf
+            for k in range(beam):
+                if tok[t, b, k] == W.EOS_ID or t == T - 1:
+                    continue
+                score[b, n], prev[b, n], nparent[b, n] = cand[t, b, k], tok[t, b, k], slot[t, b, k]
+                n += 1
+        parent = torch.from_numpy((np.arange(B)[:, None] * beam + nparent).reshape(-1).astype(np.int32)).cuda()
+    assert not set(banned) & set(tok[tok >= 0].tolist())
+    tr.close()
+
+
+def test_calls_without_an_8_bit_form():
+    w, weights, tr, w8 = _model()
+    with pytest.raises(ValueError):
+        tr.set_generator(ops.F8Weights(torch.zeros(8, 136, device="cuda")))
+    src, lens = W.make_batch(w)
+    src_d, lens_d = torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda()
+    B, S = src.shape
+    buf = tr.search_buffers(B, S, 1, 4)
+    sbuf = tr.score_buffers(B, S, 3)
+    tr.set_generator(w8)
+    with pytest.raises(_lib.OnmtError) as e:                   # allocated before: too small now
+        tr.beam_search(src_d, lens_d, buf)
+    assert e.value.code == _lib.ONMT_ESIZE
+    tgt = torch.full((B, 3), 7, dtype=torch.int32, device="cuda")
+    with pytest.raises(_lib.OnmtError) as e:
+        tr.score(src_d, lens_d, tgt, torch.full((B,), 3, dtype=torch.int32, device="cuda"), sbuf)
+    assert e.value.code == _lib.ONMT_EUNSUPPORTED
+    tr.set_generator(None)
+    tr.beam_search(src_d, lens_d, buf)
+    tr.close()
+
+
+def test_a_captured_step_with_an_8_bit_generator():
+    w, weights, tr, w8 = _model(batch=6)
+    tr.set_generator(w8)
+    tr.lib.onmt_set_validation(tr.handle, 1)
+    src, lens = W.make_batch(w)
+    B, S = src.shape
+    ws = tr.encode(torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda())
+    st = tr.decode_init(ws, B, S, 2)
+    tok = torch.full((2 * B,), W.BOS_ID, dtype=torch.int32, device="cuda")
+    tr.decode_step(ws, B, S, 2, st, tok, mode=1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = tr.decode_step(ws, B, S, 2, st, tok, mode=1)
+    for seed in range(4):
+        tok.copy_(torch.randint(4, w.tgt_vocab, (2 * B,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32))
+        graph.replay()
+        want = tr.decode_step(ws, B, S, 2, st, tok, mode=1)
+        assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+        torch.cuda.synchronize()
     tr.close()
