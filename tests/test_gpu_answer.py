@@ -59,7 +59,7 @@ def test_a_greedy_loop_with_rules():
     mask = torch.from_numpy(bits.view(np.int32)).cuda()
     row = torch.tensor([0, 1, -1, 0], dtype=torch.int32, device="cuda")
     rules = ops.LogitRules(history=history, history_len=n, no_repeat_ngram=1, mask=mask, mask_row=row,
-                           repetition=torch.full((B,), 1.5, device="cuda"))
+                           repetition=torch.full((B,), 1.5, device="cuda", dtype=torch.float32))
     ws = tr.encode(torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda())
     st = tr.decode_init(ws, B, S, 1)
     tok = torch.full((B,), W.BOS_ID, dtype=torch.int32, device="cuda")
@@ -185,7 +185,7 @@ def test_searches_with_an_8_bit_generator(beam, banned):
 def test_calls_without_an_8_bit_form():
     w, weights, tr, w8 = _model()
     with pytest.raises(ValueError):
-        tr.set_generator(ops.F8Weights(torch.zeros(8, 136, device="cuda")))
+        tr.set_generator(ops.F8Weights(torch.zeros(8, 136, device="cuda", dtype=torch.float32)))
     src, lens = W.make_batch(w)
     src_d, lens_d = torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda()
     B, S = src.shape

@@ -80,9 +80,9 @@ def weights(w):
 def make(M, N, K, kind="f32", seed=0, wkind="f32"):
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
-    x = torch.randn(M, K, generator=g, device="cuda").to(TYPES[kind])
-    w = (torch.randn(N, K, generator=g, device="cuda") * 0.1).to(TYPES[wkind])
-    return x, w, torch.randn(N, generator=g, device="cuda")
+    x = torch.randn(M, K, generator=g, device="cuda", dtype=torch.float32).to(TYPES[kind])
+    w = (torch.randn(N, K, generator=g, device="cuda", dtype=torch.float32) * 0.1).to(TYPES[wkind])
+    return x, w, torch.randn(N, generator=g, device="cuda", dtype=torch.float32)
 
 
 SIZES = [(1, 1, 1), (1, 17, 127), (3, 1000, 64), (5, 300, 128), (16, 64, 129), (17, 333, 500), (33, 4097, 260),
@@ -132,7 +132,7 @@ def test_values_are_the_definitions():
 def test_extreme_values(M, out):
     # powers far apart between blocks and rows, zero rows, infinities (the largest finite value), NaN in one row
     x, w, _ = make(M, 200, 400, seed=9)
-    x = x * torch.exp2(torch.linspace(-40, 40, M, device="cuda"))[:, None]
+    x = x * torch.exp2(torch.linspace(-40, 40, M, device="cuda", dtype=torch.float32))[:, None]
     x[:, 128:256] *= 2.0 ** -20
     x[1] = 0
     w[3] = 0
@@ -142,7 +142,7 @@ def test_extreme_values(M, out):
     y = w8.linear(x, out_dtype=TYPES[out])
     assert y[2, :3].isnan().all() and y[2, 4:].isnan().all()
     assert not y[:2].isnan().any() and not y[3:].isnan().any()
-    z = torch.zeros(M, 400, device="cuda")
+    z = torch.zeros(M, 400, device="cuda", dtype=torch.float32)
     z[0, 0] = float("inf")
     w[:, 0] = 2.0 ** -100
     w8 = weights(w)
@@ -154,8 +154,8 @@ def test_extreme_values(M, out):
 def test_strides_and_odd_addresses():
     for M, N, K in ((6, 77, 131), (150, 301, 259)):
         for kind in ("f32", "bf16"):
-            base = torch.randn(M, K + 9, device="cuda").to(TYPES[kind])
-            wbase = torch.randn(N, K + 5, device="cuda").to(TYPES[kind])
+            base = torch.randn(M, K + 9, device="cuda", dtype=torch.float32).to(TYPES[kind])
+            wbase = torch.randn(N, K + 5, device="cuda", dtype=torch.float32).to(TYPES[kind])
             x, w = base[:, 3:3 + K], wbase[:, 1:1 + K]
             w8 = weights(w)
             for out in ("f32", "bf16"):
@@ -218,6 +218,6 @@ def test_refused_tensors():
     with pytest.raises(ValueError):
         w8.linear(x, out_dtype=torch.float64)
     with pytest.raises(ValueError):
-        w8.linear(x, out=torch.empty(4, 99, device="cuda"))
+        w8.linear(x, out=torch.empty(4, 99, device="cuda", dtype=torch.float32))
     with pytest.raises(ValueError):
         ops.F8Weights(w.double())
