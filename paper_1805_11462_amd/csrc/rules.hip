@@ -74,35 +74,64 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Per token of the slice a word (occurrences in the low half, last bias entry + 1 in the high half; then the new logit); the
-// touched tokens as bits and, up to LIST of them, as a list (more: every token's bit is looked at); the tokens that would
-// end a repeated n-gram. Small enough for eight workgroups per CU, which hide each other's trips to memory.
-template <int PER>
+// What a workgroup knows about the tokens its rules name: for each a word (occurrences in the low half, last bias entry + 1 in
+// the high half; then the new logit), a list of them, bits of them, and bits of the tokens that would end a repeated n-gram.
+enum { kNoLists = 0, kLongLists = 1, kShortLists = 2 };
+constexpr int kListed = 1024;
+
+// Long lists: a word per token of the slice; the list holds up to kListed of the touched ones (more: every token's bit is looked at).
+// Small enough for eight workgroups of 4096 tokens per CU, which hide each other's trips to memory.
+template <int PER, int LISTS>
 struct RuleLds {
   static constexpr int SLICE = PER * kThreads, WORDS = SLICE / 32;
-  static constexpr int LIST = 1024;
   uint32_t word[SLICE];
-  uint16_t list[LIST];
+  uint16_t list[kListed];
   uint32_t touched[WORDS];
   uint32_t ends[WORDS];
   int n;
 };
 
-template <class S>
-__device__ __forceinline__ void touch(S& s, int o) {
+// Short lists, of at most kListed entries together: a word per touched token, found through a slot per token of the slice, which
+// needs no clearing and half the room: workgroups of 8192 tokens, six per CU.
+template <int PER>
+struct RuleLds<PER, kShortLists> {
+  static constexpr int SLICE = PER * kThreads, WORDS = SLICE / 32;
+  uint16_t slot[SLICE];
+  uint32_t word[kListed];
+  uint16_t list[kListed];
+  uint32_t touched[WORDS];
+  uint32_t ends[WORDS];
+  int n;
+};
+
+// The first to touch token o lists it.
+template <int PER>
+__device__ __forceinline__ void touch(RuleLds<PER, kLongLists>& s, int o) {
   const uint32_t bit = 1u << (o & 31);
   if (atomicOr(&s.touched[o >> 5], bit) & bit) return;
   const int at = atomicAdd(&s.n, 1);
-  if (at < s.LIST) s.list[at] = (uint16_t)o;
+  if (at < kListed) s.list[at] = (uint16_t)o;
 }
+template <int PER>
+__device__ __forceinline__ void touch(RuleLds<PER, kShortLists>& s, int o) {
+  const uint32_t bit = 1u << (o & 31);
+  if (atomicOr(&s.touched[o >> 5], bit) & bit) return;
+  const int at = atomicAdd(&s.n, 1);               // below kListed: every entry touches one token
+  s.list[at] = (uint16_t)o;
+  s.slot[o] = (uint16_t)at;
+  s.word[at] = 0;
+}
+template <int PER>
+__device__ __forceinline__ uint32_t& word_of(RuleLds<PER, kLongLists>& s, int o) { return s.word[o]; }
+template <int PER>
+__device__ __forceinline__ uint32_t& word_of(RuleLds<PER, kShortLists>& s, int o) { return s.word[s.slot[o]]; }
 
 // v = the lane's logits of row `row` under the rules, -inf past V. s: used where there is a history or a bias list. Everything
 // whose address is known at the start is loaded there (the first entries of the lists too), so that one trip to memory is
 // exposed instead of one per rule (2560 x 50000 bf16 with every rule: 236 us before).
-// LISTS: there is a history or a bias list.
-template <class T, bool LISTS, int PER, int VEC>
+template <class T, int LISTS, int PER, int VEC>
 __device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, int row, const Tokens<PER, VEC>& tk,
-                                      RuleLds<PER>& s, float (&v)[PER]) {
+                                      RuleLds<PER, LISTS>& s, float (&v)[PER]) {
   constexpr int NV = Tokens<PER, VEC>::NV, SLICE = Tokens<PER, VEC>::SLICE;
   const float ninf = -__builtin_inff();
   const int tid = threadIdx.x, width = min(SLICE, V - tk.slice0);
@@ -141,49 +170,55 @@ __device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, in
     return b[o >> 5] >> (o & 31) & ((1u << VEC) - 1);
   };
   if constexpr (LISTS) {
+    if constexpr (LISTS == kLongLists)
 #pragma unroll
-    for (int i = 0; i < PER / 4; ++i) ((uint4*)s.word)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < PER / 4; ++i) ((uint4*)s.word)[tid + i * kThreads] = make_uint4(0, 0, 0, 0);
     if (tid < s.WORDS) s.touched[tid] = s.ends[tid] = 0;
     if (tid == 0) s.n = 0;
-    lds_barrier();
-    if (q.n_bias) {
+    // f(token within the slice, entry) for every entry of a list; ahead: the thread's first entry
+    auto each = [&](const int32_t* list, int ahead, int n, auto&& f) {
       auto entry = [&](int id, int j) {
         const int o = id - tk.slice0;
-        if (id < tk.slice0 || o >= width || j >= q.n_bias) return;
-        atomicMax(&s.word[o], (uint32_t)(j + 1) << 16);
-        touch(s, o);
+        if (id >= tk.slice0 && o < width && j < n) f(o, j);
       };
-      entry(bid, tid);
-      for (int j = tid + kThreads; j < q.n_bias; j += kThreads) entry(ids[j], j);
+      entry(ahead, tid);
+      for (int j0 = kThreads; j0 < n; j0 += 4 * kThreads) {      // four loads in flight
+        int id[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int j = j0 + tid + a * kThreads;
+          id[a] = j < n ? list[j] : -1;
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) entry(id[a], j0 + tid + a * kThreads);
+      }
+    };
+    lds_barrier();
+    if constexpr (LISTS == kShortLists) {            // slots first, then what is counted in them
+      if (penalties) each(h, hid, n, [&](int o, int) { touch(s, o); });
+      if (q.n_bias) each(ids, bid, q.n_bias, [&](int o, int) { touch(s, o); });
+      lds_barrier();
+    }
+    if (q.n_bias) {
+      each(ids, bid, q.n_bias, [&](int o, int j) {
+        if constexpr (LISTS == kLongLists) touch(s, o);
+        atomicMax(&word_of(s, o), (uint32_t)(j + 1) << 16);
+      });
       lds_barrier();
     }
     if (q.history) {
       const int last = n > 0 ? h[n - 1] : 0;
-      auto entry = [&](int id, int before_it, int j) {
-        const int o = id - tk.slice0;
-        if (id < tk.slice0 || o >= width || j >= n) return;
+      each(h, hid, n, [&](int o, int j) {
         if (penalties) {
-          atomicAdd(&s.word[o], 1u);
-          touch(s, o);
+          if constexpr (LISTS == kLongLists) touch(s, o);
+          atomicAdd(&word_of(s, o), 1u);
         }
-        if (ngrams && j >= g - 1 && (g == 1 || before_it == last)) {
+        if (ngrams && j >= g - 1 && (g == 1 || (j == tid ? prev : h[j - 1]) == last)) {
           bool same = true;
           for (int i = 2; i < g && same; ++i) same = h[j - i] == h[n - i];
           if (same) atomicOr(&s.ends[o >> 5], 1u << (o & 31));
         }
-      };
-      entry(hid, prev, tid);
-      for (int j0 = kThreads; j0 < n; j0 += 4 * kThreads) {      // four loads in flight
-        int id[4], before_it[4];
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const int j = j0 + tid + a * kThreads;
-          id[a] = j < n ? h[j] : -1;
-          before_it[a] = ngrams && g > 1 && j < n ? h[j - 1] : 0;
-        }
-#pragma unroll
-        for (int a = 0; a < 4; ++a) entry(id[a], before_it[a], j0 + tid + a * kThreads);
-      }
+      });
       lds_barrier();
     }
     if (penalties || q.n_bias) {
@@ -191,29 +226,40 @@ __device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, in
       const float pres = penalties && q.presence ? q.presence[row] : 0.f;
       const float freq = penalties && q.frequency ? q.frequency[row] : 0.f;
       const float* bias = q.bias + (int64_t)row * q.bias_stride;
-      const bool listed = s.n <= s.LIST;
+      const bool listed = LISTS == kShortLists || s.n <= kListed;
       for (int i = tid; i < (listed ? s.n : SLICE); i += kThreads) {
         const int o = listed ? s.list[i] : i;
         if (!listed && !(s.touched[o >> 5] >> (o & 31) & 1)) continue;
-        const uint32_t w = s.word[o], c = w & 0xffff, j = w >> 16;
+        uint32_t& at = LISTS == kShortLists ? s.word[i] : s.word[o];
+        const uint32_t w = at, c = w & 0xffff, j = w >> 16;
         float z = to_float(x[tk.slice0 + o]);
         const float b = j ? bias[j - 1] : 0.f;
         if (c) z = penalized(z, (float)c, q.repetition != nullptr, rho, freq, pres);
         if (j) z += b;
-        s.word[o] = __builtin_bit_cast(uint32_t, z);
+        at = __builtin_bit_cast(uint32_t, z);
       }
       lds_barrier();
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
         const uint32_t b = bits_of(s.touched, u);
         if (b) {
+          const int o = tk.at(u) - tk.slice0;
 #pragma unroll
           for (int i = 0; i < VEC; i += 4) {
-            const uint4 w = *(const uint4*)&s.word[tk.at(u) - tk.slice0 + i];
-            v[u * VEC + i] = b >> i & 1 ? __builtin_bit_cast(float, w.x) : v[u * VEC + i];
-            v[u * VEC + i + 1] = b >> i & 2 ? __builtin_bit_cast(float, w.y) : v[u * VEC + i + 1];
-            v[u * VEC + i + 2] = b >> i & 4 ? __builtin_bit_cast(float, w.z) : v[u * VEC + i + 2];
-            v[u * VEC + i + 3] = b >> i & 8 ? __builtin_bit_cast(float, w.w) : v[u * VEC + i + 3];
+            uint32_t w[4];
+            if constexpr (LISTS == kShortLists) {    // slots of other tokens hold anything
+              const uint2 q = *(const uint2*)&s.slot[o + i];
+              w[0] = s.word[q.x & (kListed - 1)];
+              w[1] = s.word[q.x >> 16 & (kListed - 1)];
+              w[2] = s.word[q.y & (kListed - 1)];
+              w[3] = s.word[q.y >> 16 & (kListed - 1)];
+            } else {
+              const uint4 q = *(const uint4*)&s.word[o + i];
+              w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              v[u * VEC + i + k] = b >> (i + k) & 1 ? __builtin_bit_cast(float, w[k]) : v[u * VEC + i + k];
           }
         }
       }
@@ -233,14 +279,14 @@ __device__ __forceinline__ void ruled(const LogitRules& q, const T* x, int V, in
   }
 }
 
-template <class T, int PER, bool LISTS>
+template <class T, int PER, int LISTS>
 __global__ __launch_bounds__(kThreads) void k_rules_logits(LogitRules q, const T* x, int64_t ld, int V, int slices,
                                                            T* out, int64_t ld_out) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int row = blockIdx.x / slices;
   const Tokens<PER, kVec<T>> tk(blockIdx.x % slices);
   float v[PER];
-  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS>*)lds, v);
   T* o = out + (int64_t)row * ld_out;
 #pragma unroll
   for (int u = 0; u < tk.NV; ++u) {
@@ -274,7 +320,7 @@ __host__ __device__ inline int list_cap(int K) { return 4 * K < 32 ? 4 * K : 32;
 // more, are listed in no order. Tiles with more of them (ties) list the K largest, by K rounds of an argmax. Ranking belongs
 // to the row's merge. (2560 x 50000 bf16 at K = 5: theta bit by bit with ballots and lists ranked here took 331 scalar
 // and 357 vector instructions per wave, and either unit was as long in it as the memory.)
-template <class T, int PER, bool LISTS, bool TOP>
+template <class T, int PER, int LISTS, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const T* __restrict__ x, int64_t ld, int V, int slices,
                                                              RulePartials p) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -283,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const
   const Tokens<PER, VEC> tk(slice);
   const float ninf = -__builtin_inff();
   float v[PER];
-  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS>*)lds, v);
   const int lane = threadIdx.x & 63;
   const int tile = slice * (kThreads / kWave) + (threadIdx.x >> 6);
   if (tile >= p.ntiles) return;
@@ -465,7 +511,7 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void k_rules_merge(RulePartial
 }
 
 // log-probabilities: the logits under the rules again, less the row's logsumexp, which every wave forms from the partials.
-template <class T, int PER, bool LISTS>
+template <class T, int PER, int LISTS>
 __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, const T* x, int64_t ld, int V, int slices,
                                                               RulePartials p, float* logp, int64_t ld_out,
                                                               float* __restrict__ lse_out) {
@@ -475,7 +521,7 @@ __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, cons
   const Tokens<PER, VEC> tk(blockIdx.x % slices);
   const float ninf = -__builtin_inff();
   float v[PER];
-  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER>*)lds, v);
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS>*)lds, v);
   const float lse = row_lse(p.max + (size_t)row * p.ntiles, p.sum + (size_t)row * p.ntiles, p.ntiles);
   if (lse_out && tk.slice0 == 0 && threadIdx.x == 0) lse_out[row] = lse;
   float* o = logp + (int64_t)row * ld_out;
@@ -494,28 +540,37 @@ __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, cons
   }
 }
 
-static bool has_lists(const LogitRules& r) { return r.history || r.n_bias > 0; }
-
-// Tokens per lane: 16, or 32 where candidates are chosen among logits without lists and every CU still gets workgroups enough:
-// that halves what a tile costs beside its logits (2560 x 50000 bf16, K = 5: 65 us against 81, K = 16: 104 against 144). With
-// lists the LDS of a slice of twice the size halves the workgroups per CU (every rule: 173 us against 137); without candidates
-// there is nothing to halve (logits alone 94 us against 89).
-static int per_lane(const LogitRules& r, int N, int V, int K) {
-  const int64_t slices = (V + 32 * kThreads - 1) / (32 * kThreads) * (int64_t)N;
-  return K > 0 && !has_lists(r) && slices >= 1024 ? 32 : 16;
+static int lists_of(const LogitRules& r) {
+  if (!r.history && r.n_bias == 0) return kNoLists;
+  return (r.history ? r.max_history : 0) + r.n_bias <= kListed ? kShortLists : kLongLists;
 }
 
-// f(a null pointer of the logits' type, tokens per lane and whether there are lists as types, slices, LDS bytes)
+// Tokens per lane: 16, or 32 where that leaves several rounds of workgroups and pays: it halves what a tile costs beside its
+// logits (2560 x 50000 bf16, K = 5, no lists: 65 us against 81, every rule: 127 against 139), but not where there are neither lists
+// nor candidates (logits alone 94 us against 89), nor with long lists, whose LDS it doubles (173 us against 137), nor at fewer
+// rows (320 x 50000 fp32 with penalties 26.0 us against 24.8).
+static int per_lane(const LogitRules& r, int N, int V, int K) {
+  const int64_t slices = (V + 32 * kThreads - 1) / (32 * kThreads) * (int64_t)N;
+  const int lists = lists_of(r);
+  return slices >= 4096 && lists != kLongLists && (K > 0 || lists == kShortLists) ? 32 : 16;
+}
+
+// f(a null pointer of the logits' type, tokens per lane and the kind of lists as types, slices, LDS bytes)
 template <class F>
 static hipError_t by_type(const LogitRules& r, const LogitMat& m, int K, F&& f) {
   auto run = [&](auto* t, auto per, auto lists) {
-    constexpr int P = decltype(per)::value;
-    f(t, per, lists, (m.V + P * kThreads - 1) / (P * kThreads), decltype(lists)::value ? (int)sizeof(RuleLds<P>) : 0);
+    constexpr int P = decltype(per)::value, L = decltype(lists)::value;
+    f(t, per, lists, (m.V + P * kThreads - 1) / (P * kThreads), L ? (int)sizeof(RuleLds<P, L>) : 0);
   };
   auto g = [&](auto* t) {
-    if (has_lists(r)) run(t, Const<16>{}, Const<1>{});
-    else if (per_lane(r, m.N, m.V, K) == 16) run(t, Const<16>{}, Const<0>{});
-    else run(t, Const<32>{}, Const<0>{});
+    const bool wide = per_lane(r, m.N, m.V, K) == 32;
+    switch (lists_of(r)) {
+      case kNoLists:
+        return wide ? run(t, Const<32>{}, Const<kNoLists>{}) : run(t, Const<16>{}, Const<kNoLists>{});
+      case kShortLists:
+        if (wide) return run(t, Const<32>{}, Const<kShortLists>{});
+    }
+    return run(t, Const<16>{}, Const<kLongLists>{});
   };
   if (m.dtype == kF32) g((float*)nullptr);
   else if (m.dtype == kBF16) g((bf16_t*)nullptr);
@@ -535,7 +590,7 @@ size_t rules_ws(int N, int V, int K) { return partials_layout(N, V, K, 16, nullp
 #define ONMT_TYPES(t, per, lists)                         \
   using T = std::remove_pointer_t<decltype(t)>;           \
   constexpr int P = decltype(per)::value;                 \
-  constexpr bool L = decltype(lists)::value != 0
+  constexpr int L = decltype(lists)::value
 
 hipError_t rules_logits(const LogitRules& r, const LogitMat& m, void* out, int64_t ld_out, hipStream_t st) {
   return by_type(r, m, 0, [&](auto* t, auto per, auto lists, int sl, int lds) {

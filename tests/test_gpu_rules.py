@@ -63,10 +63,14 @@ def ruled(x, history=None, history_len=None, repetition=None, presence=None, fre
     return x
 
 
-def check(logits, K=5, modes=(0, 1, 2), **rules):
-    """All modes of one call against the plain implementation."""
+def check(logits, K=5, modes=(0, 1, 2), times=1, **rules):
+    """All modes of one call against the plain implementation. times: with that many copies of the rows, one after the other."""
     host = {k: (v.cpu().numpy() if isinstance(v, torch.Tensor) else v) for k, v in rules.items()}
-    x = ruled(logits.float().cpu().numpy(), **host)
+    x = np.tile(ruled(logits.float().cpu().numpy(), **host), (times, 1))
+    if times > 1:
+        logits = logits.repeat(times, 1)
+        rules = {k: (v.repeat(times, *[1] * (v.dim() - 1)) if isinstance(v, torch.Tensor) and k != "mask" else v)
+                 for k, v in rules.items()}
     q = ops.LogitRules(**rules) if rules else None
     if 2 in modes:
         out, ids, lse = ops.constrain(logits, q, mode=2)
@@ -134,7 +138,7 @@ def everything(N, V, T=40, nbias=6, tables=3, seed=0, ngram=2):
 def logits_of(N, V, kind, seed=1):
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
-    return (3 * torch.randn(N, V, generator=g, device="cuda")).to(TYPES[kind])
+    return (3 * torch.randn(N, V, generator=g, device="cuda", dtype=torch.float32)).to(TYPES[kind])
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
@@ -146,10 +150,36 @@ def test_vocabularies(V, kind):
     check(x, K=5, **everything(5, V))
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("times,V,T", [(600, 37, 40), (600, 300, 5), (300, 9001, 40), (600, 8192, 100), (600, 70, 1100)])
+def test_many_rows(times, V, T, kind):
+    print(f"[case] {7 * times} rows of {V} {kind}, history {T}", flush=True)
+    check(logits_of(7, V, kind), K=16, times=times)
+    check(logits_of(7, V, kind), K=5, times=times, **everything(7, V, T=T, nbias=20, ngram=3))
+
+
+@pytest.mark.parametrize("times", [1, 1400])
+@pytest.mark.parametrize("T,nbias", [(1024, 0), (0, 1024), (1000, 24), (1000, 25), (2, 3000)])
+def test_lists_of_many_different_tokens(times, T, nbias):
+    """Every entry another token, all in one slice."""
+    V, N = 4000, 3
+    g = np.random.default_rng(T + nbias)
+    rules = {}
+    if T:
+        h = np.stack([g.permutation(V)[:T] for _ in range(N)]).astype(np.int32)
+        rules.update(history=torch.from_numpy(h).cuda(), history_len=torch.full((N,), T, dtype=torch.int32, device="cuda"),
+                     presence=torch.ones(N, dtype=torch.float32, device="cuda"))
+    if nbias:
+        ids = np.stack([g.permutation(V)[:nbias] for _ in range(N)]).astype(np.int32)
+        rules.update(bias_ids=torch.from_numpy(ids).cuda(), bias=logits_of(N, nbias, "f32", seed=3))
+    check(logits_of(N, V, "f32"), modes=(1, 2), times=times, **rules)
+
+
 @pytest.mark.parametrize("K", [1, 2, 5, 8, 16])
 def test_widths(K):
     for kind in ("f32", "bf16"):
-        check(logits_of(9, 6000, kind, seed=K), K=K, modes=(1,), **everything(9, 6000, seed=K))
+        for times in (1, 500):
+            check(logits_of(9, 6000, kind, seed=K), K=K, modes=(1,), times=times, **everything(9, 6000, seed=K))
 
 
 @pytest.mark.parametrize("ngram", [1, 2, 3, 5, 60])
@@ -222,7 +252,7 @@ def test_strides_odd_addresses_and_in_place():
         want = ops.constrain(x, q, mode=2)[0]
         logp = ops.constrain(x, q, mode=0)[0]
         keep = base.clone()
-        wide = torch.full((N, V + 4), 9.0, device="cuda")
+        wide = torch.full((N, V + 4), 9.0, device="cuda", dtype=torch.float32)
         ops.constrain(x, q, mode=0, out=wide[:, 1:1 + V])
         assert torch.equal(wide[:, 1:1 + V], logp) and (wide[:, 0] == 9).all() and (wide[:, 1 + V:] == 9).all()
         if kind == "f32":
