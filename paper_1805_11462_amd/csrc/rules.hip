@@ -402,21 +402,42 @@ __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const
   }
 }
 
-// The row's logsumexp from its partials, in every lane.
-__device__ __forceinline__ float row_lse(const float* __restrict__ mx, const float* __restrict__ sm, int ntiles) {
-  const int lane = threadIdx.x & 63;
-  const float ninf = -__builtin_inff();
-  float m = ninf, s = 0.f;
-  for (int t = lane; t < ntiles; t += kWave) m = fmaxf(m, mx[t]);
-  m = wave_max(m);
-  const float shift = m > ninf ? m : 0.f;
-  for (int t = lane; t < ntiles; t += kWave) s += sm[t] * __expf(mx[t] - shift);
-  return shift + logf(wave_sum(s));
-}
+// A row's partials, lane l those of tiles l + 64 j: loaded at once, those past the first kAhead per lane where they are needed.
+struct RowTiles {
+  static constexpr int kAhead = 4;
+  const float *mx, *sm;
+  int ntiles;
+  float m[kAhead], s[kAhead];
+  __device__ __forceinline__ RowTiles(const RulePartials& p, int row)
+      : mx(p.max + (size_t)row * p.ntiles), sm(p.sum + (size_t)row * p.ntiles), ntiles(p.ntiles) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int t = lane + j * kWave;
+      m[j] = t < ntiles ? mx[t] : -__builtin_inff();
+      s[j] = t < ntiles ? sm[t] : 0.f;
+    }
+  }
+  // The largest value of the lane's tiles.
+  __device__ __forceinline__ float lane_max() const {
+    float r = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+    for (int t = (threadIdx.x & 63) + kAhead * kWave; t < ntiles; t += kWave) r = fmaxf(r, mx[t]);
+    return r;
+  }
+  // The row's logsumexp, in every lane; lmax: lane_max().
+  __device__ __forceinline__ float lse(float lmax) const {
+    const float top = wave_max(lmax), shift = top > -__builtin_inff() ? top : 0.f;
+    float r = 0.f;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) r += s[j] * __expf(m[j] - shift);
+    for (int t = (threadIdx.x & 63) + kAhead * kWave; t < ntiles; t += kWave) r += sm[t] * __expf(mx[t] - shift);
+    return shift + logf(wave_sum(r));
+  }
+};
 
 // One wave per row: the lists of the tiles whose maximum reaches the K-th largest tile maximum hold the row's K largest values;
 // those that reach it too are ranked against each other. Where ties make that too many, K rounds of an argmax over all lists.
-constexpr int kMergeWaves = 4, kMergeTiles = 256, kMergeCands = 256;
+constexpr int kMergeWaves = 1, kMergeTiles = 256, kMergeCands = 256;
 
 __global__ __launch_bounds__(kMergeWaves * kWave) void k_rules_merge(RulePartials p, int N, float* __restrict__ out,
                                                                      int32_t* __restrict__ out_id, float* __restrict__ out_lse) {
@@ -427,23 +448,27 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void k_rules_merge(RulePartial
   if (row >= N) return;
   const float ninf = -__builtin_inff();
   const int K = p.K, cap = list_cap(K);
-  const float* mx = p.max + (size_t)row * p.ntiles;
+  const RowTiles tiles(p, row);
+  const float* mx = tiles.mx;
   const int* cnt = p.count + (size_t)row * p.ntiles;
   const uint2* lists = p.list + (size_t)row * p.ntiles * cap;
-  const float lse = row_lse(mx, p.sum + (size_t)row * p.ntiles, p.ntiles);
-  float c = ninf, theta = ninf;
-  for (int t = lane; t < p.ntiles; t += kWave) c = fmaxf(c, mx[t]);
+  float c = tiles.lane_max(), theta = ninf;
+  const float lse = tiles.lse(c);
   for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
   const unsigned long long below = lane == 0 ? 0ull : (~0ull >> (64 - lane));
   int nq = 0, n = 0;
-  for (int t0 = 0; t0 < p.ntiles; t0 += kWave) {
-    const int t = t0 + lane;
-    const bool q = t < p.ntiles && mx[t] >= theta && mx[t] > ninf;
+  auto qualify = [&](int t, float m) {
+    const bool q = m >= theta && m > ninf;
     const unsigned long long who = __ballot(q);
     const int pos = nq + __popcll(who & below);
     if (q && pos < kMergeTiles) qt[w][pos] = t;
     nq += __popcll(who);
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < RowTiles::kAhead; ++j)
+    if (j * kWave < p.ntiles) qualify(lane + j * kWave, tiles.m[j]);
+  for (int t0 = RowTiles::kAhead * kWave; t0 < p.ntiles; t0 += kWave)
+    qualify(t0 + lane, t0 + lane < p.ntiles ? mx[t0 + lane] : ninf);
   __builtin_amdgcn_wave_barrier();
   if (nq <= kMergeTiles)
     for (int s0 = 0; s0 < nq * cap && n <= kMergeCands; s0 += kWave) {
@@ -520,9 +545,10 @@ __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, cons
   constexpr int VEC = 4, NV = PER / VEC;       // 16-byte stores
   const Tokens<PER, VEC> tk(blockIdx.x % slices);
   const float ninf = -__builtin_inff();
+  const RowTiles tiles(p, row);
   float v[PER];
   ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS>*)lds, v);
-  const float lse = row_lse(p.max + (size_t)row * p.ntiles, p.sum + (size_t)row * p.ntiles, p.ntiles);
+  const float lse = tiles.lse(tiles.lane_max());
   if (lse_out && tk.slice0 == 0 && threadIdx.x == 0) lse_out[row] = lse;
   float* o = logp + (int64_t)row * ld_out;
 #pragma unroll
