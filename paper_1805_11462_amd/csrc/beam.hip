@@ -12,15 +12,6 @@ namespace onmt {
 // ------------------------------------------------------------------ partials of given logits
 // Half a wave per (row, 128-column tile), four logits per lane: the tile's largest logit, the sum of exp(logit - that) and
 // the largest that the filters allow, as the generator's epilogue leaves them. Bound by memory (320 x 50000: 64 MB).
-__device__ inline float half_max(float v) {
-  v = fmaxf(v, dpp_move<0x111, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x112, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x114, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x118, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x142, 0xa>(v, v));
-  return (threadIdx.x & 32) ? readlane_f(v, 63) : readlane_f(v, 31);
-}
-
 __global__ __launch_bounds__(256) void k_tile_partials(GenParams p, int M, int pairs) {
   typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;

@@ -341,7 +341,7 @@ struct F8Tile {
 
 template <class C, class T>
 __global__ __launch_bounds__(C::NT) void k_f8_wide(F8Mat x, F8Mat w, int M, int N, const float* __restrict__ bias,
-                                                   T* __restrict__ out, int64_t ld, int nm, int nn, int band) {
+                                                   T* __restrict__ out, int64_t ld, int nm, int nn, int band, F8Partials part) {
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int TM = C::TM, TN = C::TN, W = C::WM * C::WN;
   __shared__ __attribute__((aligned(16))) char lds[C::LDS];
@@ -478,6 +478,25 @@ __global__ __launch_bounds__(C::NT) void k_f8_wide(F8Mat x, F8Mat w, int M, int 
         const int m = at.rb0 * 16 + r / (8 * TM) * (16 * TM) + pass * (8 * TM) + r % (8 * TM);
         typedef T vec __attribute__((ext_vector_type(VEC)));
         const vec v = *(const vec*)(mid + (r * CH + ((lane % CH) ^ (r & 7))) * 16);
+        if constexpr (EXACT && C::BN == 128) {   // half a wave holds the row's 128 columns
+          if (part.max) {
+            const float ninf = -__builtin_inff();
+            float z[VEC], top = ninf, sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+              z[j] = n + j < N ? v[j] : ninf;
+              top = fmaxf(top, z[j]);
+            }
+            top = half_max(top);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum += top > ninf ? __expf(z[j] - top) : 0.f;
+            sum = group_sum<32>(sum);
+            if ((lane & 31) == 31 && m < M) {
+              part.max[(size_t)m * part.ntiles + at.cb0 / 8] = top;
+              part.sum[(size_t)m * part.ntiles + at.cb0 / 8] = sum;
+            }
+          }
+        }
         if (m < M) {
           T* p = out + (int64_t)m * ld + n;
           if (n + VEC <= N) {
@@ -542,16 +561,19 @@ static void launch_few(const void* x, int64_t ldx, int M, const F8Mat& w, int N,
 }
 
 template <class C, class T>
-static void launch_wide(const F8Mat& x, int M, const F8Mat& w, int N, const float* bias, void* out, int64_t ld, hipStream_t st) {
+static void launch_wide(const F8Mat& x, int M, const F8Mat& w, int N, const float* bias, void* out, int64_t ld, const F8Partials& part,
+                        hipStream_t st) {
   const int nm = (M + C::BM - 1) / C::BM, nn = (N + C::BN - 1) / C::BN;
   const int slots = min(C::SLOTS, (nm * nn + 7) / 8 * 8);         // whole rounds of the XCDs
-  hipLaunchKernelGGL((k_f8_wide<C, T>), dim3(slots), dim3(C::NT), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nn, 8);
+  hipLaunchKernelGGL((k_f8_wide<C, T>), dim3(slots), dim3(C::NT), 0, st, x, w, M, N, bias, (T*)out, ld, nm, nn, 8, part);
 }
 
 size_t f8_linear_ws(int M, int cols) { return few_rows(M, cols, true) ? 0 : f8_data_bytes(M, cols) + f8_exp_bytes(M, cols); }
 
 hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out,
-                     int out_dtype, int64_t ld, void* ws, hipStream_t st) {
+                     int out_dtype, int64_t ld, void* ws, hipStream_t st, F8Partials* part) {
+  const F8Partials p = part ? *part : F8Partials{};
+  if (part) *part = F8Partials{};
   if (const int tm = few_rows(M, cols, out_dtype == kF32))
     return f8_type(dtype, [&](auto* tx) {
       f8_type(out_dtype, [&](auto* to) {
@@ -569,8 +591,9 @@ hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& 
   return f8_type(out_dtype, [&](auto* to) {
     using T = ONMT_TYPE(to);
     if constexpr (sizeof(T) == 2)
-      if (M > 192) return launch_wide<F8Tile<8, 4, 2, 4, 256>, T>(xm, M, w, N, bias, out, ld, st);
-    launch_wide<F8Tile<4, 4, 2, 2, 512>, T>(xm, M, w, N, bias, out, ld, st);
+      if (M > 192) return launch_wide<F8Tile<8, 4, 2, 4, 256>, T>(xm, M, w, N, bias, out, ld, p, st);
+    launch_wide<F8Tile<4, 4, 2, 2, 512>, T>(xm, M, w, N, bias, out, ld, p, st);
+    if (part && sizeof(T) == 4) *part = p;
   });
 }
 

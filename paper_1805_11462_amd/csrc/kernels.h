@@ -290,10 +290,17 @@ inline F8Mat f8_mat(void* buf, int64_t rows, int cols) {
 }
 hipError_t f8_pack(const void* x, int dtype, int64_t ld, int rows, int cols, const F8Mat& out, hipStream_t st);
 hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld, hipStream_t st);
-// out [M, N] (row stride ld) = x w^T + bias (optional), x [M, cols] rounded to e4m3 in ws (f8_linear_ws bytes) first.
+// The generator's partials of fp32 results: largest value and sum of exp per row and 128 columns, [M, ntiles].
+struct F8Partials {
+  float* max;
+  float* sum;
+  int ntiles;
+};
+// out [M, N] (row stride ld) = x w^T + bias (optional), x [M, cols] rounded to e4m3 in ws (f8_linear_ws bytes) first. part
+// (optional): partials that are wanted too; its pointers are null afterwards if this product has not written them.
 size_t f8_linear_ws(int M, int cols);
 hipError_t f8_linear(const void* x, int dtype, int64_t ldx, int M, const F8Mat& w, int N, int cols, const float* bias, void* out,
-                     int out_dtype, int64_t ld, void* ws, hipStream_t st);
+                     int out_dtype, int64_t ld, void* ws, hipStream_t st, F8Partials* part = nullptr);
 
 // Rules on logits (rules.hip); the pointers of rules that are off are null.
 struct LogitRules {

@@ -1233,9 +1233,11 @@ int decode_compute(onmt_model* m, const EncWs& w, int B, int S, int K, const Sta
     part = gen_partials(gp);
     if (timing) time_begin(m, st);
     if (d.gen8) {
+      F8Partials fp{gp.pmax, gp.psum, gp.ntiles};
+      const bool fused = mode != 4 && !gp.pfmax;         // filters need the largest allowed logits too
       HIP_TRY(f8_linear(out.feed, kF32, d.H, N, f8_mat((void*)m->W_8, d.Vt, d.H), d.Vt, d.H, m->b_s, gp.logits, kF32, gp.ld_logits,
-                        sw.act8, st));
-      if (mode != 4) HIP_TRY(tile_partials(gp, N, st));
+                        sw.act8, st, fused ? &fp : nullptr));
+      if (mode != 4 && !(fused && fp.max)) HIP_TRY(tile_partials(gp, N, st));
     } else {
       HIP_TRY(gemm_gen(Split16{out.feed16, N, d.kb(d.H)}, m->W_s, d.wterms, gp, st));
     }
