@@ -276,18 +276,19 @@ enum { ONMT_F32 = 0, ONMT_BF16 = 1, ONMT_F16 = 2 };
 /* ---- Products with 8-bit floating-point weights -------------------------------------------------------
  * A matrix is held as e4m3 values (4 exponent and 3 mantissa bits, largest 448) with a power of two for each block of 128
  * columns of a row (the last may be shorter): the smallest, from 2^-127 on, that brings the block's largest entry to 448 or less.
- * Entries are rounded to the nearest value, ties to even: off by at most 2^-4 of themselves, entries below 2^-14 of the
- * block's largest by at most 2^-18 of it. Entries beyond +-1.875 2^127, infinities among them, count as that; a NaN
+ * Entries are rounded to the nearest value, ties to even: off by at most 2^-4 of themselves, entries below 2^-13 of the
+ * block's largest by at most 2^-17 of it. Entries beyond +-1.875 2^127, infinities among them, count as that; a NaN
  * stays one and makes the results it takes part in NaN.
  *
  * onmt_f8_pack writes w [rows, cols] in that form into packed (onmt_f8_bytes(rows, cols) bytes, 0 for sizes out of range; 16-byte
  * aligned), onmt_f8_unpack the values that it stands for. onmt_f8_linear computes
  *   out[m, n] = sum_k x8[m, k] w8[n, k] + bias[n]      (m < M, n < rows, k < cols; bias fp32 or NULL)
  * with x8 = x in the same form, accumulated in fp32 and rounded once to out's type (bf16 and fp16 results: blocks of 128
- * products are summed by the 8-bit matrix instruction, off by some 1.5e-5 of a sum's rms). ws holds onmt_f8_linear_ws_bytes(M, cols) bytes
- * of scratch, 16-byte aligned (where that is 0, ws may be NULL); out overlaps neither x nor ws nor packed. All are asynchronous on the stream and may be captured;
- * calls that share no ws and no output may run at the same time. Sizes: up to 2^20 columns, 2^24 blocks of 16 rows x 128 columns per operand
- * and 2^24 tiles of 16 x 64 outputs (ONMT_EUNSUPPORTED beyond). */
+ * products are summed by the 8-bit matrix instruction, off by some 1.5e-5 of a sum's rms; values and sums below 2^-126 may
+ * count as 0). ws holds onmt_f8_linear_ws_bytes(M, cols) bytes of scratch, 16-byte aligned (where that is 0, ws may be NULL);
+ * out and ws overlap neither an input nor each other. All are asynchronous on the stream and may be captured; calls that share
+ * no ws and no output may run at the same time. Sizes: up to 2^20 columns, 2^24 blocks of 16 rows x 128 columns per operand
+ * and 2^30 tiles of 16 x 64 outputs (ONMT_EUNSUPPORTED beyond). */
 size_t onmt_f8_bytes(int rows, int cols);
 int onmt_f8_pack(const void* w, int dtype, int64_t ld, int rows, int cols, void* packed, size_t packed_bytes, void* stream);
 int onmt_f8_unpack(const void* packed, size_t packed_bytes, int rows, int cols, float* out, int64_t ld_out, void* stream);
@@ -310,10 +311,11 @@ int onmt_set_generator(onmt_model* model, const void* packed, size_t packed_byte
  *   v in the row's bias list:  x = x + bias of the last entry that names v
  *   no_repeat_ngram = n > 0 and the history holds the n-gram (its last n - 1 ids, v):  x = -inf
  *   mask bit v & 31 of word v >> 5 is 0:  x = -inf, whatever it was (NaN too)
- * All pointers are device pointers; a NULL one switches its rule off (without a history nothing is repeated). history [N, max_history] (row stride history_stride) holds
- * history_len[r] ids of row r (clamped to [0, max_history]; what lies behind does not matter). Ids outside [0, V) in histories and
- * bias lists match no token (in n-grams they are ids like others). bias_ids, bias: [N, n_bias], row stride bias_stride.
- * max_history and n_bias are at most 65535 (ONMT_EUNSUPPORTED beyond).
+ * All pointers are device pointers; a NULL one switches its rule off (without a history nothing is repeated).
+ * history [N, max_history] (row stride history_stride) holds history_len[r] ids of row r (clamped to [0, max_history]; what lies
+ * behind does not matter). Ids outside [0, V) in histories and bias lists match no token (in n-grams they are ids like
+ * others). bias_ids, bias: [N, n_bias], row stride bias_stride. max_history and n_bias are at most 65535
+ * (ONMT_EUNSUPPORTED beyond).
  * mask: n_masks tables of ceil(V / 32) words (row stride mask_stride); row r uses table mask_row[r] (any negative number: none;
  * n_masks or more: every token is forbidden), or table r where mask_row is NULL (n_masks >= N). */
 typedef struct {
@@ -341,9 +343,9 @@ typedef struct {
  *   rounded to the logits' type. lse [N] (optional; NULL in mode 2) = logsumexp of x over the row, -inf where no token is allowed.
  * A NaN or +inf among the allowed logits makes the row's lse and its log-probs NaN; a NaN is never among the K largest.
  * In modes 0 (fp32 logits) and 2, out may be the logits themselves (same pointer and stride); otherwise it does not overlap
- * them. ws holds onmt_constrain_ws_bytes(N, V, mode, K) bytes, 16-byte aligned (0 and NULL in mode 2). V <= 2^20 and at most 2^23
- * slices of 4096 logits (ONMT_EUNSUPPORTED beyond). Asynchronous on the stream, may be captured; calls that share no ws and no
- * output may run at the same time. */
+ * them, nor do ws, ids or lse overlap any input. ws holds onmt_constrain_ws_bytes(N, V, mode, K) bytes, 16-byte aligned (0 and
+ * NULL in mode 2). V <= 2^20 and at most 2^23 slices of 4096 logits (ONMT_EUNSUPPORTED beyond). Asynchronous on the stream, may
+ * be captured; calls that share no ws and no output may run at the same time. */
 size_t onmt_constrain_ws_bytes(int N, int V, int mode, int K);
 int onmt_constrain(const onmt_logit_rules* rules, const void* logits, int dtype, int64_t ld, int N, int V, int mode, int K,
                    void* out, int64_t ld_out, int32_t* ids, float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -3,9 +3,11 @@
 
 #include <cmath>
 
+#include "answer.h"
 #include "common.h"
 #include "kernels.h"
 #include "split16.h"
+#include "types.h"
 
 namespace onmt {
 

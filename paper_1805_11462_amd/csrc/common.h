@@ -78,15 +78,6 @@ __device__ inline float wave_max(float v) {
   v = fmaxf(v, dpp_move<0x143, 0xc>(v, v));
   return readlane_f(v, 63);
 }
-// The largest value of each half of the wave, in its lanes.
-__device__ inline float half_max(float v) {
-  v = fmaxf(v, dpp_move<0x111, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x112, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x114, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x118, 0xf>(v, v));
-  v = fmaxf(v, dpp_move<0x142, 0xa>(v, v));
-  return (threadIdx.x & 32) ? readlane_f(v, 63) : readlane_f(v, 31);
-}
 __device__ inline float wave_sum(float v) { return readlane_f(group_sum<64>(v), 63); }
 
 }  // namespace onmt

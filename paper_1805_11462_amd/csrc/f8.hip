@@ -2,12 +2,12 @@
 //
 // A block whose largest finite entry is a = f 2^p (1 <= f < 2) is stored as q = e4m3(x 2^-e), rounded to nearest even, with
 // e = p - 8 where f <= 1.75 and p - 7 else: the smallest power that brings a to 448, e4m3's largest value, or less. An entry is
-// off by at most half an e4m3 step, 2^-4 of its value, down to 2^-14 of the block's largest (2^-10 2^e below). A power of two
+// off by at most half an e4m3 step, 2^-4 of its value, down to 2^-13 of the block's largest (2^-10 2^e below). A power of two
 // costs no accuracy against a scale of full precision (the steps of a floating-point type move with it), and the
 // matrix instruction takes it as an operand: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies one 128-column block of 16 rows of either
 // side and scales it by 2^(ex + ew) of its rows and columns, at twice the rate of the 16-bit ones. But it aligns the 128 products
 // to the largest before it adds them and drops what falls below some 17 bits: sums of normal values are off by 1.5e-5 of their
-// rms (measured; 16x16x32_fp8_fp8 the same), which 16-bit results do not see (their own rounding is 2^-9 or 2^-12) and fp32 results do.
+// rms (measured; 16x16x32_fp8_fp8 the same), which 16-bit results do not see (their own rounding is up to 2^-8 or 2^-11) and fp32 results do.
 // Those multiply the same e4m3 values as bf16, exact with their powers included (v_cvt_scalef32_pk_bf16_fp8), in
 // v_mfma_f32_16x16x32_bf16: 2e-8 to 1e-7.
 //
@@ -21,9 +21,9 @@
 
 #include <type_traits>
 
+#include "answer.h"
 #include "common.h"
 #include "gemm_device.h"
-#include "kernels.h"
 #include "types.h"
 
 namespace onmt {
@@ -111,18 +111,17 @@ __global__ __launch_bounds__(256) void k_f8_pack(const T* __restrict__ x, int64_
 }
 
 __global__ __launch_bounds__(256) void k_f8_unpack(F8Mat w, int rows, int cols, float* __restrict__ out, int64_t ld) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int quads = (cols + 3) / 4;
-  const int64_t row = i / quads;
-  if (row >= rows) return;
-  const int r = (int)row, c = (int)(i % quads) * 4;
-  const int rb = r / 16, kb = c / kF8Block, g = c % kF8Block / 32, o = c % 32;
-  const int word = *(const int*)(w.data + ((size_t)kb * w.rblocks + rb) * kF8Frag + (o >= 16 ? kF8Frag / 2 : 0) +
-                                 (r % 16 + 16 * g) * 16 + o % 16);
-  const int e = (int)(((const uint8_t*)(w.exps + ((size_t)(kb / 4) * w.rblocks + rb) * 16 + r % 16))[kb & 3]) - kF8One;
-  const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(word, 0), __builtin_amdgcn_cvt_f32_fp8(word, 1),
-                      __builtin_amdgcn_cvt_f32_fp8(word, 2), __builtin_amdgcn_cvt_f32_fp8(word, 3)};
-  for (int j = 0; j < 4 && c + j < cols; ++j) out[(int64_t)r * ld + c + j] = ldexpf(v[j], e);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * quads; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / quads), c = (int)(i % quads) * 4;
+    const int rb = r / 16, kb = c / kF8Block, g = c % kF8Block / 32, o = c % 32;
+    const int word = *(const int*)(w.data + ((size_t)kb * w.rblocks + rb) * kF8Frag + (o >= 16 ? kF8Frag / 2 : 0) +
+                                   (r % 16 + 16 * g) * 16 + o % 16);
+    const int e = (int)(((const uint8_t*)(w.exps + ((size_t)(kb / 4) * w.rblocks + rb) * 16 + r % 16))[kb & 3]) - kF8One;
+    const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(word, 0), __builtin_amdgcn_cvt_f32_fp8(word, 1),
+                        __builtin_amdgcn_cvt_f32_fp8(word, 2), __builtin_amdgcn_cvt_f32_fp8(word, 3)};
+    for (int j = 0; j < 4 && c + j < cols; ++j) out[(int64_t)r * ld + c + j] = ldexpf(v[j], e);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------- products
@@ -535,8 +534,8 @@ hipError_t f8_pack(const void* x, int dtype, int64_t ld, int rows, int cols, con
 }
 
 hipError_t f8_unpack(const F8Mat& w, int rows, int cols, float* out, int64_t ld, hipStream_t st) {
-  const int64_t n = (int64_t)rows * ((cols + 3) / 4);
-  hipLaunchKernelGGL(k_f8_unpack, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, w, rows, cols, out, ld);
+  const int64_t nb = ((int64_t)rows * ((cols + 3) / 4) + 255) / 256;
+  hipLaunchKernelGGL(k_f8_unpack, dim3((unsigned)(nb < 65536 ? nb : 65536)), dim3(256), 0, st, w, rows, cols, out, ld);
   return hipGetLastError();
 }
 

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "../../include/onmt.h"
+#include "answer.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -1272,7 +1273,8 @@ int check_beam(const onmt_model* m, int S, int K) {
 
 // ------------------------------------------------------------------ matrices of a caller's type, rules on logits
 constexpr int64_t kF8MaxBlocks = 1 << 24;
-constexpr int kF8MaxCols = 1 << 20;            // the products' offsets within a tile's rows are 32-bit byte counts
+constexpr int64_t kF8MaxTiles = 1 << 30;
+constexpr int kF8MaxCols = 1 << 20;
 constexpr int kMaxRuleVocab = 1 << 20, kMaxRuleList = 65535;      // lists: counts and entries share a word
 
 int64_t f8_blocks(int64_t rows, int64_t cols) { return ((rows + 15) / 16) * ((cols + kF8Block - 1) / kF8Block); }
@@ -1743,15 +1745,17 @@ int onmt_f8_linear(const void* x, int dtype, int64_t ldx, int M, const void* pac
   if (rc || (rc = check_matrix("out", out, out_dtype, ld_out, M, rows)) || (rc = check_packed(packed, packed_bytes, rows, cols)))
     return rc;
   if ((uintptr_t)bias % sizeof(float)) return fail(ONMT_EINVAL, "bias is not aligned to its elements");
-  if (!f8_fits(M, cols) || ((M + 15) / 16) * (int64_t)((rows + 63) / 64) > kF8MaxBlocks)
+  if (!f8_fits(M, cols) || ((M + 15) / 16) * (int64_t)((rows + 63) / 64) > kF8MaxTiles)
     return fail(ONMT_EUNSUPPORTED, "a product of %d x %d by %d rows is too large", M, cols, rows);
   const size_t need = onmt_f8_linear_ws_bytes(M, cols);
   if (need && (!ws || (uintptr_t)ws % 16)) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
   if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
-  const Span so = span(out, out_dtype, ld_out, M, rows);
-  if (so.meets(span(x, dtype, ldx, M, cols)) || so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need}) ||
-      so.meets(Span{(uintptr_t)packed, (uintptr_t)packed + onmt_f8_bytes(rows, cols)}))
-    return fail(ONMT_EINVAL, "out overlaps x, ws or packed");
+  const Span so = span(out, out_dtype, ld_out, M, rows), sx = span(x, dtype, ldx, M, cols);
+  const Span sw{(uintptr_t)ws, (uintptr_t)ws + need}, sp{(uintptr_t)packed, (uintptr_t)packed + onmt_f8_bytes(rows, cols)};
+  if (so.meets(sx) || so.meets(sw) || so.meets(sp) || (bias && so.meets(span(bias, ONMT_F32, rows, 1, rows))))
+    return fail(ONMT_EINVAL, "out overlaps x, ws, packed or bias");
+  if (sw.meets(sx) || sw.meets(sp) || (bias && sw.meets(span(bias, ONMT_F32, rows, 1, rows))))
+    return fail(ONMT_EINVAL, "ws overlaps x, packed or bias");
   hipStream_t st = (hipStream_t)stream;
   HIP_TRY(f8_linear(x, dtype, ldx, M, f8_mat((void*)packed, rows, cols), rows, cols, bias, out, out_dtype, ld_out, ws, st));
   return ONMT_OK;
@@ -1802,7 +1806,8 @@ int onmt_constrain(const onmt_logit_rules* rules, const void* logits, int dtype,
   if (!ws || (uintptr_t)ws % 16) return fail(ONMT_EINVAL, "ws must be a 16-byte aligned device buffer");
   const size_t need = onmt_constrain_ws_bytes(N, V, mode, K);
   if (ws_bytes < need) return fail(ONMT_ESIZE, "ws holds %zu bytes, %zu are needed", ws_bytes, need);
-  if (so.meets(Span{(uintptr_t)ws, (uintptr_t)ws + need})) return fail(ONMT_EINVAL, "out overlaps ws");
+  const Span sw{(uintptr_t)ws, (uintptr_t)ws + need};
+  if (so.meets(sw) || sw.meets(span(logits, dtype, ld, N, V))) return fail(ONMT_EINVAL, "ws overlaps out or the logits");
   HIP_TRY(mode == 0 ? rules_log_probs(r, m, ws, (float*)out, ld_out, lse, st)
                     : rules_top(r, m, K, ws, (float*)out, ids, lse, st));
   return ONMT_OK;

@@ -17,8 +17,8 @@
 #include <cstddef>
 #include <type_traits>
 
+#include "answer.h"
 #include "common.h"
-#include "kernels.h"
 #include "types.h"
 
 namespace onmt {

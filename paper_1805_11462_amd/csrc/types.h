@@ -1,8 +1,11 @@
-// Element types of a caller's matrices, and accesses to them that need no more than the element's own alignment.
+// Element types of a caller's matrices, accesses to them that need no more than the element's own alignment, and what else the
+// kernels on them share.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "common.h"
 
 namespace onmt {
 
@@ -40,6 +43,16 @@ __device__ __forceinline__ void store_vec(T* p, const float* v) {
 #pragma unroll
   for (int i = 0; i < kVec<T>; ++i) x[i] = (T)v[i];
   *(typename VecOf<T>::type*)p = x;
+}
+
+// The largest value of each half of the wave, in its lanes.
+__device__ inline float half_max(float v) {
+  v = fmaxf(v, dpp_move<0x111, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x112, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x114, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x118, 0xf>(v, v));
+  v = fmaxf(v, dpp_move<0x142, 0xa>(v, v));
+  return (threadIdx.x & 32) ? readlane_f(v, 63) : readlane_f(v, 31);
 }
 
 }  // namespace onmt

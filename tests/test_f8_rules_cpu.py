@@ -47,7 +47,9 @@ def linear(**kw):
     (dict(M=100, ws_bytes=64), _lib.ONMT_ESIZE),
     # out over x, over the workspace, over the weights
     (dict(out=P), _lib.ONMT_EINVAL), (dict(out=P + 5 * 500 * 4 - 4), _lib.ONMT_EINVAL), (dict(M=100, out=WS), _lib.ONMT_EINVAL),
-    (dict(out=W + 64), _lib.ONMT_EINVAL),
+    (dict(out=W + 64), _lib.ONMT_EINVAL), (dict(bias=OUT + 4 * 4999), _lib.ONMT_EINVAL),
+    # the workspace over x, over the weights, over the bias
+    (dict(M=100, ws=P), _lib.ONMT_EINVAL), (dict(M=100, ws=W), _lib.ONMT_EINVAL), (dict(M=100, bias=WS), _lib.ONMT_EINVAL),
     (dict(M=1 << 30, ldx=500), _lib.ONMT_EUNSUPPORTED),
 ])
 def test_linear_refusals(kw, code):
@@ -92,6 +94,7 @@ def constrain(rules=None, **kw):
     (dict(V=4, ld=4), _lib.ONMT_EINVAL), (dict(ids=None), _lib.ONMT_EINVAL), (dict(ids=W + 1), _lib.ONMT_EINVAL),
     (dict(ld_out=6), _lib.ONMT_EINVAL), (dict(out=None), _lib.ONMT_EINVAL), (dict(ws=None), _lib.ONMT_EINVAL),
     (dict(ws_bytes=8), _lib.ONMT_ESIZE), (dict(out=P), _lib.ONMT_EINVAL), (dict(out=WS), _lib.ONMT_EINVAL),
+    (dict(ws=P), _lib.ONMT_EINVAL),
     (dict(mode=2, ld_out=1000, lse=W), _lib.ONMT_EINVAL),
     # in place needs the same pointer, stride and type
     (dict(mode=2, out=P + 4, ld_out=1000), _lib.ONMT_EINVAL), (dict(mode=2, out=P, ld_out=1001), _lib.ONMT_EINVAL),
@@ -110,10 +113,12 @@ def test_constrain_refusals(kw, code):
     dict(history=P + 2, history_len=P, history_stride=10, max_history=10),
     dict(no_repeat_ngram=-1),
     dict(n_bias=-1), dict(n_bias=3, bias_ids=P, bias_stride=3), dict(n_bias=3, bias_ids=P, bias=P, bias_stride=2),
+    dict(history=P, history_len=P, history_stride=1 << 20, max_history=65536), dict(n_bias=65536, bias_ids=P, bias=P, bias_stride=65536),
     dict(mask=P, mask_stride=31, n_masks=4), dict(mask=P, mask_stride=32, n_masks=0, mask_row=P),
     dict(mask=P, mask_stride=32, n_masks=3),                                             # a table per row: four are needed
     dict(mask=P, mask_stride=32, n_masks=1, mask_row=P + 1),
 ])
 def test_rules_refusals(rules):
-    assert constrain(rules) == _lib.ONMT_EINVAL
+    long = rules.get("max_history", 0) > 65535 or rules.get("n_bias", 0) > 65535
+    assert constrain(rules) == (_lib.ONMT_EUNSUPPORTED if long else _lib.ONMT_EINVAL)
     assert len(_lib.load().onmt_last_error()) > 0
