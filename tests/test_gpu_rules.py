@@ -158,6 +158,19 @@ def test_many_rows(times, V, T, kind):
     check(logits_of(7, V, kind), K=5, times=times, **everything(7, V, T=T, nbias=20, ngram=3))
 
 
+@pytest.mark.parametrize("T", [40, 1500])
+@pytest.mark.parametrize("V", [4097, 16383, 16384, 16385, 32767, 32768, 32769])
+def test_rows_at_the_sizes_a_workgroup_holds(V, T):
+    for kind in TYPES:
+        print(f"[case] V {V} {kind}, history {T}", flush=True)
+        check(logits_of(6, V, kind), K=7, modes=(0, 1), **everything(6, V, T=T, nbias=30, ngram=3))
+
+
+def test_many_rows_beyond_what_a_workgroup_holds():
+    check(logits_of(7, 33001, "bf16"), modes=(0, 1), times=130, **everything(7, 33001))
+    check(logits_of(7, 33001, "f32"), modes=(0,), times=130)
+
+
 @pytest.mark.parametrize("times", [1, 1400])
 @pytest.mark.parametrize("T,nbias", [(1024, 0), (0, 1024), (1000, 24), (1000, 25), (2, 3000)])
 def test_lists_of_many_different_tokens(times, T, nbias):
