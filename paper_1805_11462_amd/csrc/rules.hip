@@ -14,6 +14,7 @@
 // bounds it is memory: each logit is read once (twice for log-probabilities of rows past a workgroup's registers, the second
 // time from the caches where the batch fits them) and each output written once.
 
+#include <algorithm>
 #include <cstddef>
 #include <type_traits>
 
@@ -315,12 +316,87 @@ struct RulePartials {
 // Entries of a tile's list: as many values as may pass its bound, or the K largest.
 __host__ __device__ inline int list_cap(int K) { return 4 * K < 32 ? 4 * K : 32; }
 
-// Rows' partials: a tile's largest value and the sum of exp(v - that) (NaN where one is; a +inf makes it NaN too). TOP: the
-// values that can be among the row's K largest, at most list_cap(K) of each tile. theta, the K-th largest of the maxima of
-// 16 groups of four lanes (K > 8: of the 64 lanes), is at most the tile's K-th largest value: those that reach it, K or a few
-// more, are listed in no order. Tiles with more of them (ties) list the K largest, by K rounds of an argmax. Ranking belongs
-// to the row's merge. (2560 x 50000 bf16 at K = 5: theta bit by bit with ballots and lists ranked here took 331 scalar
-// and 357 vector instructions per wave, and either unit was as long in it as the memory.)
+// The lane's share of a wave's maximum and, with that in every lane, the sum of exp(v - maximum) (NaN where one is; a +inf makes
+// it NaN too).
+template <int PER>
+__device__ __forceinline__ float lane_max(const float (&v)[PER]) {
+  float m = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) m = fmaxf(m, v[i]);
+  return m;
+}
+template <int PER>
+__device__ __forceinline__ float sum_exp(const float (&v)[PER], float top) {
+  const float shift = top > -__builtin_inff() ? top : 0.f;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) s += __expf(v[i] - shift);
+  return wave_sum(s);
+}
+
+// Lists the values of a wave's tile that can be among the row's K largest, at most list_cap(K); how many they are. m: the
+// lane's largest. theta, the K-th largest of the maxima of 16 groups of four lanes (K > 8: of the 64 lanes), is at most the
+// tile's K-th largest value: those that reach it, K or a few more, are listed in no order. Tiles with more of them (ties)
+// list the K largest, by K rounds of an argmax. Ranking belongs to the row's merge. (2560 x 50000 bf16 at K = 5: theta bit by
+// bit with ballots and lists ranked here took 331 scalar and 357 vector instructions per wave, and either unit was as long in
+// it as the memory.)
+template <int PER, int VEC, int THREADS>
+__device__ __forceinline__ int list_top(const float (&v)[PER], float m, int K, const Tokens<PER, VEC, THREADS>& tk, uint2* list) {
+  const float ninf = -__builtin_inff();
+  const int lane = threadIdx.x & 63, cap = list_cap(K);
+  auto id_of = [&](int i) { return tk.at(i / VEC) + i % VEC; };
+  int n = 0;
+  float theta = ninf;
+  if (K <= 8) {
+    float c = fmaxf(m, __shfl_xor(m, 16, kWave));
+    c = fmaxf(c, __shfl_xor(c, 32, kWave));      // every row of 16 lanes holds the 16 groups' maxima
+    for (int k = 0; k < 4 * K; k += taken(c, theta)) theta = row_max(c);
+  } else {
+    float c = m;
+    for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
+  }
+  theta = fmaxf(theta, -3.402823466e38f);        // -inf is no candidate
+  const unsigned long long below = lane == 0 ? 0ull : (~0ull >> (64 - lane));
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool keep = v[i] >= theta;
+    const unsigned long long who = __ballot(keep);
+    if (who) {
+      const int pos = n + __popcll(who & below);
+      if (keep && pos < cap) list[pos] = make_uint2(__builtin_bit_cast(uint32_t, v[i]), (uint32_t)id_of(i));
+      n += __popcll(who);
+    }
+  }
+  if (n > cap) {
+    float pv = __builtin_inff();
+    int pi = -1;
+    for (n = 0; n < K; ++n) {
+      float bv = ninf;
+      int bi = kNoId;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (v[i] > ninf && before(pv, pi, v[i], id_of(i)) && before(v[i], id_of(i), bv, bi)) {
+          bv = v[i];
+          bi = id_of(i);
+        }
+#pragma unroll
+      for (int d = kWave / 2; d > 0; d >>= 1) {
+        const float ov = __shfl_xor(bv, d, kWave);
+        const int oi = __shfl_xor(bi, d, kWave);
+        if (before(ov, oi, bv, bi)) {
+          bv = ov;
+          bi = oi;
+        }
+      }
+      if (lane == 0) list[n] = make_uint2(__builtin_bit_cast(uint32_t, bv), (uint32_t)bi);
+      pv = bv;
+      pi = bi;
+    }
+  }
+  return n;
+}
+
+// Rows' partials: a tile's largest value and sum of exp and, TOP, its list.
 template <class T, int PER, int LISTS, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const T* __restrict__ x, int64_t ld, int V, int slices,
                                                              RulePartials p) {
@@ -334,68 +410,10 @@ __global__ __launch_bounds__(kThreads) void k_rules_partials(LogitRules q, const
   const int lane = threadIdx.x & 63;
   const int tile = slice * (kThreads / kWave) + (threadIdx.x >> 6);
   if (tile >= p.ntiles) return;
-  float m = ninf;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) m = fmaxf(m, v[i]);
-  const float top = wave_max(m), shift = top > ninf ? top : 0.f;
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) s += __expf(v[i] - shift);
-  s = wave_sum(s);
+  const float m = lane_max(v), top = wave_max(m), s = sum_exp(v, top);
   const size_t o = (size_t)row * p.ntiles + tile;
   int n = 0;
-  if constexpr (TOP) {
-    const int K = p.K, cap = list_cap(K);
-    auto id_of = [&](int i) { return tk.at(i / VEC) + i % VEC; };
-    float theta = ninf;
-    if (K <= 8) {
-      float c = fmaxf(m, __shfl_xor(m, 16, kWave));
-      c = fmaxf(c, __shfl_xor(c, 32, kWave));      // every row of 16 lanes holds the 16 groups' maxima
-      for (int k = 0; k < 4 * K; k += taken(c, theta)) theta = row_max(c);
-    } else {
-      float c = m;
-      for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
-    }
-    theta = fmaxf(theta, -3.402823466e38f);        // -inf is no candidate
-    const unsigned long long below = lane == 0 ? 0ull : (~0ull >> (64 - lane));
-    uint2* list = p.list + o * cap;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool keep = v[i] >= theta;
-      const unsigned long long who = __ballot(keep);
-      if (who) {
-        const int pos = n + __popcll(who & below);
-        if (keep && pos < cap) list[pos] = make_uint2(__builtin_bit_cast(uint32_t, v[i]), (uint32_t)id_of(i));
-        n += __popcll(who);
-      }
-    }
-    if (n > cap) {
-      float pv = __builtin_inff();
-      int pi = -1;
-      for (n = 0; n < K; ++n) {
-        float bv = ninf;
-        int bi = kNoId;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (v[i] > ninf && before(pv, pi, v[i], id_of(i)) && before(v[i], id_of(i), bv, bi)) {
-            bv = v[i];
-            bi = id_of(i);
-          }
-#pragma unroll
-        for (int d = kWave / 2; d > 0; d >>= 1) {
-          const float ov = __shfl_xor(bv, d, kWave);
-          const int oi = __shfl_xor(bi, d, kWave);
-          if (before(ov, oi, bv, bi)) {
-            bv = ov;
-            bi = oi;
-          }
-        }
-        if (lane == 0) list[n] = make_uint2(__builtin_bit_cast(uint32_t, bv), (uint32_t)bi);
-        pv = bv;
-        pi = bi;
-      }
-    }
-  }
+  if constexpr (TOP) n = list_top(v, m, p.K, tk, p.list + o * list_cap(p.K));
   if (lane == 0) {
     p.max[o] = top;
     p.sum[o] = s;
@@ -567,39 +585,49 @@ __global__ __launch_bounds__(kThreads) void k_rules_log_probs(LogitRules q, cons
   }
 }
 
-// The same where a workgroup holds the whole row in registers: one launch that reads every logit once. 512 x 32000 bf16 with
-// penalties and biases 21 us against 39 in two passes (24.7 against 47 fp32 logits; 17 against 24 without rules), 5.4 against 5.2
-// for a single row without rules. Rows of 50000 would leave one workgroup per CU, whose waves then wait for each other: 43 us
-// against 54 at 512 of them, but 16 against 14 at 64 and 131 against 137 at 1280, so those take two passes.
+// Where a workgroup holds the whole row in registers, one launch does it all and reads every logit once. Log-probabilities of
+// 512 x 32000 bf16 with penalties and biases 21 us against 39 in two passes (24.7 against 47 fp32 logits; 17 against 24 without
+// rules), 5.4 against 5.2 for a single row without rules. Rows of 50000 would leave one workgroup per CU, whose waves then wait
+// for each other: 43 us against 54 at 512 of them, but 16 against 14 at 64 and 131 against 137 at 1280, so those take two passes.
 constexpr int kRowThreads = 1024, kMaxRow = 32 * kRowThreads;
+
+// What the waves of a row tell each other, in the rules' LDS when those are through; cand: room for every wave's list.
+template <int THREADS>
+struct RowLds {
+  static constexpr int WAVES = THREADS / kWave, CANDS = WAVES * 32;
+  float max[WAVES], sum[WAVES];
+  int count[WAVES];
+  int n;
+  uint2 list[CANDS], cand[CANDS];
+};
+
+// The row's logsumexp from its waves' largest values and sums; wmax: lane l's that of wave l.
+template <int THREADS>
+__device__ __forceinline__ float row_lse(const RowLds<THREADS>& s, float wmax) {
+  const int lane = threadIdx.x & 63;
+  const float top = wave_max(wmax), shift = top > -__builtin_inff() ? top : 0.f;
+  return shift + logf(wave_sum(lane < s.WAVES ? s.sum[lane] * __expf(wmax - shift) : 0.f));
+}
 
 template <class T, int PER, int LISTS, int THREADS>
 __global__ __launch_bounds__(THREADS, LISTS == kLongLists && PER > 16 ? 4 : 8) void k_rules_row_log_probs(
     LogitRules q, const T* x, int64_t ld, int V, float* logp, int64_t ld_out, float* __restrict__ lse_out) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  constexpr int VEC = 4, NV = PER / VEC, WAVES = THREADS / kWave;
-  __shared__ float wm[WAVES], ws[WAVES];
+  constexpr int VEC = 4, NV = PER / VEC;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const Tokens<PER, VEC, THREADS> tk(0);
   const float ninf = -__builtin_inff();
   float v[PER];
   ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS, THREADS>*)lds, v);
-  float m = ninf, s = 0.f;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) m = fmaxf(m, v[i]);
-  m = wave_max(m);
-  const float shift = m > ninf ? m : 0.f;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) s += __expf(v[i] - shift);
-  s = wave_sum(s);
+  RowLds<THREADS>& s = *(RowLds<THREADS>*)lds;
+  const float m = wave_max(lane_max(v)), sum = sum_exp(v, m);
+  if (LISTS) lds_barrier();
   if (lane == 0) {
-    wm[threadIdx.x >> 6] = m;
-    ws[threadIdx.x >> 6] = s;
+    s.max[threadIdx.x >> 6] = m;
+    s.sum[threadIdx.x >> 6] = sum;
   }
   lds_barrier();
-  const float cm = lane < WAVES ? wm[lane] : ninf;
-  const float top = wave_max(cm), to = top > ninf ? top : 0.f;
-  const float lse = to + logf(wave_sum(lane < WAVES ? ws[lane] * __expf(cm - to) : 0.f));
+  const float lse = row_lse(s, lane < s.WAVES ? s.max[lane] : ninf);
   if (lse_out && threadIdx.x == 0) lse_out[row] = lse;
   float* o = logp + (int64_t)row * ld_out;
 #pragma unroll
@@ -615,6 +643,56 @@ __global__ __launch_bounds__(THREADS, LISTS == kLongLists && PER > 16 ? 4 : 8) v
         if (t + i < V) o[t + i] = v[u * VEC + i];
     }
   }
+}
+
+// The K largest: every wave lists its candidates, those of them that reach the K-th largest wave maximum are ranked. At 16 tokens
+// per lane; with 32 the listing runs out of registers (512 x 32000 bf16 with penalties and biases 52 us against 24 in two launches).
+template <class T, int PER, int LISTS, int THREADS>
+__global__ __launch_bounds__(THREADS, 8) void k_rules_row_top(
+    LogitRules q, const T* __restrict__ x, int64_t ld, int V, int K, float* __restrict__ out, int32_t* __restrict__ out_id,
+    float* __restrict__ lse_out) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const Tokens<PER, kVec<T>, THREADS> tk(0);
+  const float ninf = -__builtin_inff();
+  float v[PER];
+  ruled<T, LISTS>(q, x + (int64_t)row * ld, V, row, tk, *(RuleLds<PER, LISTS, THREADS>*)lds, v);
+  RowLds<THREADS>& s = *(RowLds<THREADS>*)lds;
+  const float m = lane_max(v), top = wave_max(m), sum = sum_exp(v, top);
+  if (LISTS) lds_barrier();
+  const int mine = list_top(v, m, K, tk, &s.list[w * 32]);
+  if (lane == 0) {
+    s.max[w] = top;
+    s.sum[w] = sum;
+    s.count[w] = mine;
+  }
+  if (tid == 0) s.n = 0;
+  lds_barrier();
+  const float wmax = lane < s.WAVES ? s.max[lane] : ninf, lse = row_lse(s, wmax);
+  float c = wmax, theta = ninf;
+  for (int k = 0; k < K; k += taken(c, theta)) theta = wave_max(c);
+  if (tid < s.CANDS && tid % 32 < s.count[tid / 32]) {
+    const uint2 a = s.list[tid];
+    if (__builtin_bit_cast(float, a.x) >= theta) s.cand[atomicAdd(&s.n, 1)] = a;      // in any order: ranks follow from value and id
+  }
+  lds_barrier();
+  const int n = s.n;
+  float* o = out + (size_t)row * K;
+  int32_t* oi = out_id + (size_t)row * K;
+  if (tid < n) {
+    const uint2 a = s.cand[tid];
+    const float z = __builtin_bit_cast(float, a.x);
+    int rank = 0;
+    for (int d = 0; d < n; ++d) rank += before(__builtin_bit_cast(float, s.cand[d].x), (int)s.cand[d].y, z, (int)a.y) ? 1 : 0;
+    if (rank < K) {
+      o[rank] = z - lse;
+      oi[rank] = (int)a.y;
+    }
+  } else if (tid < K) {
+    o[tid] = ninf;
+    oi[tid] = kNoId;
+  }
+  if (lse_out && tid == 0) lse_out[row] = lse;
 }
 
 static int lists_of(const LogitRules& r) {
@@ -687,23 +765,14 @@ static hipError_t partials(const LogitRules& r, const LogitMat& m, int K, void* 
   });
 }
 
-hipError_t rules_top(const LogitRules& r, const LogitMat& m, int K, void* ws, float* out, int32_t* ids, float* lse,
-                     hipStream_t st) {
-  RulePartials p;
-  const hipError_t e = partials(r, m, K, ws, &p, st);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_rules_merge, dim3((m.N + kMergeWaves - 1) / kMergeWaves), dim3(kMergeWaves * kWave), 0, st, p, m.N, out,
-                     ids, lse);
-  return hipGetLastError();
-}
-
 // f(a null pointer of the logits' type, tokens per lane, the kind of lists and threads as types, LDS bytes) for rows of at most
 // kMaxRow logits, the smallest workgroup that holds one.
 template <class F>
 static hipError_t by_row(const LogitRules& r, const LogitMat& m, F&& f) {
   auto run = [&](auto* t, auto per, auto lists, auto threads) {
     constexpr int P = decltype(per)::value, L = decltype(lists)::value, D = decltype(threads)::value;
-    f(t, per, lists, threads, L ? (int)sizeof(RuleLds<P, L, D>) : 0);
+    const int rules = L ? (int)sizeof(RuleLds<P, L, D>) : 0;
+    f(t, per, lists, threads, std::max(rules, (int)sizeof(RowLds<D>)));
   };
   auto h = [&](auto* t, auto per, auto threads) {
     switch (lists_of(r)) {
@@ -720,6 +789,27 @@ static hipError_t by_row(const LogitRules& r, const LogitMat& m, F&& f) {
   if (m.dtype == kF32) g((float*)nullptr);
   else if (m.dtype == kBF16) g((bf16_t*)nullptr);
   else g((f16_t*)nullptr);
+  return hipGetLastError();
+}
+
+hipError_t rules_top(const LogitRules& r, const LogitMat& m, int K, void* ws, float* out, int32_t* ids, float* lse,
+                     hipStream_t st) {
+  // One launch for rows of a small workgroup (8 x 1000 fp32 4.6 us against 6.8, with short lists 7.7 against 9.4), and for those of
+  // a large one while every row has a CU (64 x 16384 bf16 6.9 against 8.2; but 1280 rows 22 against 20: the rows' ranking has
+  // nothing to hide behind).
+  if (m.V <= 16 * kThreads || (m.V <= 16 * kRowThreads && m.N <= 256))
+    return by_row(r, m, [&](auto* t, auto per, auto lists, auto threads, int lds) {
+      ONMT_TYPES(t, per, lists);
+      constexpr int D = decltype(threads)::value;
+      if constexpr (P == 16)
+        hipLaunchKernelGGL((k_rules_row_top<T, P, L, D>), dim3(m.N), dim3(D), lds, st, r, (const T*)m.x, m.ld, m.V, K, out, ids,
+                           lse);
+    });
+  RulePartials p;
+  const hipError_t e = partials(r, m, K, ws, &p, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_rules_merge, dim3((m.N + kMergeWaves - 1) / kMergeWaves), dim3(kMergeWaves * kWave), 0, st, p, m.N, out,
+                     ids, lse);
   return hipGetLastError();
 }
 

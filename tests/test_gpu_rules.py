@@ -166,6 +166,18 @@ def test_rows_at_the_sizes_a_workgroup_holds(V, T):
         check(logits_of(6, V, kind), K=7, modes=(0, 1), **everything(6, V, T=T, nbias=30, ngram=3))
 
 
+@pytest.mark.parametrize("V", [700, 4096, 4097, 16384])
+def test_ties_and_few_tokens_in_one_launch(V):
+    """Whole rows of one value, of two, and with fewer tokens than K, at every width."""
+    x = torch.zeros(4, V, device="cuda", dtype=torch.float32)
+    x[1, ::3] = 1.0
+    x[2, 3:] = -float("inf")
+    x[3] = -float("inf")
+    for kind in TYPES:
+        for K in (1, 8, 9, 16):
+            check(x.to(TYPES[kind]), K=K, modes=(0, 1))
+
+
 def test_many_rows_beyond_what_a_workgroup_holds():
     check(logits_of(7, 33001, "bf16"), modes=(0, 1), times=130, **everything(7, 33001))
     check(logits_of(7, 33001, "f32"), modes=(0,), times=130)
