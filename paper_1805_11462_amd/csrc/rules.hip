@@ -6,8 +6,9 @@
 // is 0, gets -inf whatever it was.
 //
 // A workgroup takes 4096 consecutive tokens of a row (8192 in large batches; the whole row where its registers hold one) and
-// every wave 1024 of them, 16 per lane, in 16-byte accesses. The rules name tokens, not places, and few of them: the occurrences of a history's tokens in the slice are counted in LDS (integer
-// atomics, so their order does not matter), the first to touch a token lists it, and one thread per listed token then forms
+// every wave 1024 of them, 16 per lane, in 16-byte accesses. The rules name tokens, not places, and few of them: the
+// occurrences of a history's tokens in the slice are counted in LDS (integer atomics, so their order does not matter), the
+// first to touch a token lists it, and one thread per listed token then forms
 // its new logit, which the lane that holds the token fetches where a bitmap says so. Bias lists go the same way with an atomic
 // maximum of entry indices. (Every lane looking up a count for each of its 16 tokens, divisions and all, took
 // 322 us at 2560 x 50000 bf16 where memory alone takes 50.) The logits are loaded before that and wait in registers. What
